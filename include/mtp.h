@@ -430,6 +430,190 @@ int mtp_nar_run(mtp_ctx* ctx);
 int mtp_nar_get_codes(mtp_ctx* ctx, int32_t* codes);
 int mtp_nar_get_logits(mtp_ctx* ctx, int stage, float* logits);
 
+/* ---- Paged serving operators --------------------------------------------
+ * Context-free calls for programs that keep a batch's cache themselves: block
+ * tables and slots from request lengths, cache writes, attention over the
+ * cache, beam selection and the page copies that beams need.  Every pointer
+ * inside an argument struct is a DEVICE pointer on the current device; the
+ * struct itself is host memory, read before the call returns.  The work is
+ * enqueued on `hip_stream` (a hipStream_t, NULL = the null stream) without
+ * host synchronisation, allocation or state kept between calls, so a call may
+ * be captured into a graph; a workspace holds nothing between calls and must
+ * not be shared by calls in flight.  Lengths, tables and slots live on the
+ * device and are checked there: whatever they hold, no call reads or writes
+ * outside the buffers described here.  MTP_EINVAL: a NULL or misaligned
+ * pointer, a size outside the stated range; MTP_ENOMEM: workspace_bytes below
+ * what the *_workspace_size call reports; MTP_EHIP: a launch failed.
+ * Nothing is launched when a call is refused.  Sizes of 0 rows, tokens or
+ * requests are accepted and do nothing.
+ *
+ * A cache (one layer) is num_pages pages of 16 tokens, in the format of a
+ * context's own pool: page p holds [K, V][n_kv_heads] blocks of 16 * head_dim
+ * elements; a K block is [16 slots][head_dim], a V block [head_dim][16 slots]
+ * for bf16 caches and [16 slots][head_dim] for fp32 ones.  Slot s of the cache
+ * is slot s % 16 of page s / 16. */
+typedef struct mtp_cache {
+    void*   pool;         /* num_pages * 2 * n_kv_heads * 16 * head_dim elements, 16-byte aligned */
+    int32_t dtype;        /* MTP_DTYPE_*                                       */
+    int32_t num_pages;    /* 1 .. 2^27 - 1                                     */
+    int32_t n_kv_heads;   /* 1 .. 1024                                         */
+    int32_t head_dim;     /* 64 or 128                                         */
+} mtp_cache;
+
+/* Block tables and slot maps from lengths.  Row c continues the sequence of
+ * row p = parent[c] (c itself with parent NULL): it has p's len[p] cached
+ * tokens, in the pages table_in[p][0 .. ceil(len[p] / 16)), and takes add[c]
+ * more.  table[c] gets p's full pages (shared by every row that continues p),
+ * p's partly filled last page for the lowest such row and a fresh page for the
+ * others (whose copies[c] names the pair: source page, fresh page; -1, -1
+ * otherwise), fresh pages for the rest, and -1 behind the last page.  Fresh
+ * pages are the lowest-numbered ones that no row keeps, handed out in row and
+ * page order: a page that no row names any more is free again, with no other
+ * bookkeeping.  Also written: row_start[n_rows + 1], the exclusive sums of
+ * add; kv_len[c] = len[p] + add[c]; for the i-th new token of row c, at
+ * t = row_start[c] + i, slots[t] (its cache slot) and positions[t] =
+ * len[p] + i, both -1 behind the last token; status[4], whole counts of this
+ * call: [0] fresh pages that the pool did not have (their entries and slots
+ * are -1), [1] rows whose parent, length or add is outside its range (taken as
+ * empty), [2] kept table entries outside [0, num_pages) (kept as -1), [3] new
+ * tokens behind max_tokens (no slot).
+ * Two rows of table_in must not hold the same partly filled last page unless
+ * they are not both continued.  table may be table_in when parent is NULL;
+ * every other pair of arrays must be disjoint.  0 <= n_rows <= 4096,
+ * 1 <= max_pages <= 65536, 1 <= num_pages < 2^27, 0 <= max_tokens < 2^31;
+ * len[p] + add[c] <= 16 * max_pages.  Arrays are 4-byte aligned, the
+ * workspace (about num_pages / 8 + 16 n_rows bytes) 256-byte. */
+typedef struct mtp_plan_args {
+    int32_t n_rows, max_pages, num_pages, max_tokens;
+    const int32_t* parent;      /* [n_rows], or NULL                           */
+    const int32_t* len;         /* [n_rows] cached tokens                      */
+    const int32_t* add;         /* [n_rows] new tokens                         */
+    const int32_t* table_in;    /* [n_rows][max_pages]                         */
+    int32_t* table;             /* [n_rows][max_pages]                         */
+    int32_t* row_start;         /* [n_rows + 1]                                */
+    int32_t* kv_len;            /* [n_rows]                                    */
+    int32_t* slots;             /* [max_tokens]                                */
+    int32_t* positions;         /* [max_tokens]                                */
+    int32_t* copies;            /* [n_rows][2]                                 */
+    int32_t* status;            /* [4]                                         */
+    void* workspace;
+    uint64_t workspace_bytes;
+} mtp_plan_args;
+int mtp_pages_plan_workspace_size(const mtp_plan_args* args, uint64_t* bytes);
+int mtp_pages_plan(const mtp_plan_args* args, void* hip_stream);
+
+/* Writes the keys and values of n_tokens tokens into the cache: token t's
+ * head h, k[t * k_stride + h * head_dim ..] and v likewise, in the cache's
+ * type, at slots[t]; a slot outside [0, 16 * num_pages) is skipped.  Slots
+ * must differ (of two equal ones either token may stay).  Strides are in
+ * elements, at least n_kv_heads * head_dim; k, v and the strides' bytes are
+ * multiples of 16. */
+typedef struct mtp_write_args {
+    mtp_cache cache;
+    int32_t n_tokens;
+    const int32_t* slots;       /* [n_tokens]                                  */
+    const void* k;
+    const void* v;
+    int64_t k_stride, v_stride;
+} mtp_write_args;
+int mtp_pages_write(const mtp_write_args* args, void* hip_stream);
+
+/* Copies whole pages in every layer's cache (layer l at pool + l *
+ * layer_stride bytes): copies[i] = (source, target) as mtp_pages_plan writes
+ * them; a pair with a page outside [0, num_pages) or with source == target is
+ * skipped.  Targets must differ, and no target may be a source.  page_bytes
+ * and layer_stride are multiples of 16; layer_stride >= num_pages *
+ * page_bytes with more than one layer. */
+typedef struct mtp_copy_args {
+    void* pool;                 /* 16-byte aligned                             */
+    uint64_t page_bytes, layer_stride;
+    int32_t n_layers, num_pages, n_copies;
+    const int32_t* copies;      /* [n_copies][2]                               */
+} mtp_copy_args;
+int mtp_pages_copy(const mtp_copy_args* args, void* hip_stream);
+
+/* Attention of new tokens over the cache.  Row c's queries are the tokens
+ * t = row_start[c] .. row_start[c + 1) of q (token t's head h at q[t *
+ * q_stride + h * head_dim ..], the cache's type), its keys and values the
+ * kv_len[c] first slots of its pages table[c].  Query head h reads KV head
+ * h / (n_heads / n_kv_heads).  out[t][h] = sum_j p_j V[j] with p = softmax
+ * over the visible j of scale * q . K[j]:
+ *   MTP_ATTN_CAUSAL  the queries are the row's last positions: query i of n
+ *                    sits at kv_len - n + i and sees the positions up to its
+ *                    own, and with window > 0 only the last `window` of them
+ *                    (itself included);
+ *   MTP_ATTN_FULL    every query sees all kv_len positions (cross attention to
+ *                    an encoder's states, or a bidirectional block).
+ * A query that sees nothing gets zeros.  Positions in a page outside [0,
+ * num_pages) are seen by nobody, and what is not seen never matters, infinite
+ * or NaN.  Tokens outside every row keep what out holds.  Lengths are clamped
+ * to [0, 16 * max_pages], row_start to [0, n_tokens]; row_start must not
+ * decrease.  max_kv is a hint, the longest kv_len to expect (0: 16 *
+ * max_pages): it sizes the split of the keys over workgroups, and longer rows
+ * are right, only slower.  Scores, softmax and sums are float32; with a bf16
+ * cache the probabilities are rounded to bf16 for the product with V.
+ * 0 <= n_rows <= 4096, 1 <= max_pages <= 65536, 0 <= n_tokens < 2^24,
+ * n_heads a multiple of n_kv_heads up to 1024, window >= 0, scale finite.
+ * q, out and the bytes of their strides are multiples of 16, the strides at
+ * least n_heads * head_dim; out must not overlap another operand.  The
+ * workspace is 256-byte aligned (NULL when the size call reports 0). */
+#define MTP_ATTN_CAUSAL  0
+#define MTP_ATTN_FULL    1
+typedef struct mtp_attention_args {
+    mtp_cache cache;
+    int32_t n_rows, max_pages, n_tokens, n_heads;
+    int32_t mode, window, max_kv;
+    float scale;
+    const int32_t* table;       /* [n_rows][max_pages]                         */
+    const int32_t* row_start;   /* [n_rows + 1]                                */
+    const int32_t* kv_len;      /* [n_rows]                                    */
+    const void* q;
+    void* out;
+    int64_t q_stride, out_stride;
+    void* workspace;
+    uint64_t workspace_bytes;
+} mtp_attention_args;
+int mtp_pages_attention_workspace_size(const mtp_attention_args* args, uint64_t* bytes);
+int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream);
+
+/* Beam search's selection.  Request r has `beams` beams, row w = r * beams +
+ * b with logits[w * ld ..] (float32 [vocab]), score[w] (the sum of its tokens'
+ * log probabilities), len[w] tokens and done[w].  An unfinished beam's
+ * candidates are its `vocab` continuations, score[w] + log softmax(logits)[v]
+ * at length len[w] + 1, with eos_id masked (before the softmax) while len[w] <
+ * eos_min; a finished beam's only one is itself, as token eos_id with its
+ * score and length kept.  The request's next beams are its `beams` best
+ * candidates by score / max(length, 1)^alpha, the best first; equal ones in
+ * the order of b * vocab + v.  A logit that is NaN counts as -infinity, and so
+ * does a candidate whose score is NaN or +infinity; candidates of -infinity
+ * come last.
+ * Scores and ranks are formed in float64 from float32 exponentials summed in
+ * float64, a beam's own candidates ordered by their logits.  Written per next
+ * beam: out_score (float32), out_len, out_done (done before, or the token is
+ * eos_id), out_parent (the row w it continues, as mtp_pages_plan's parent) and
+ * out_token.  The out arrays may be the in arrays of the same name.
+ * 0 <= n_requests, n_requests * beams <= 65536, 1 <= beams <= 32, 1 <= vocab
+ * < 2^24, ld >= vocab, eos_id in [0, vocab), alpha finite and >= 0; logits
+ * 4-byte, workspace 256-byte aligned. */
+typedef struct mtp_beam_args {
+    int32_t n_requests, beams, vocab, eos_id, eos_min;
+    float alpha;
+    const float* logits;
+    int64_t ld;
+    const float* score;         /* each array: [n_requests * beams]            */
+    const int32_t* len;
+    const int32_t* done;
+    float* out_score;
+    int32_t* out_len;
+    int32_t* out_done;
+    int32_t* out_parent;
+    int32_t* out_token;
+    void* workspace;
+    uint64_t workspace_bytes;
+} mtp_beam_args;
+int mtp_beam_select_workspace_size(const mtp_beam_args* args, uint64_t* bytes);
+int mtp_beam_select(const mtp_beam_args* args, void* hip_stream);
+
 /* Drops all sequence state (the next call must be mtp_prefill). */
 int mtp_reset(mtp_ctx* ctx);
 void mtp_destroy(mtp_ctx* ctx);

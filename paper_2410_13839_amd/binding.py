@@ -37,10 +37,14 @@ EXPORTED = ["mtp_query_sizes", "mtp_weight_offset", "mtp_create", "mtp_prefill",
             "mtp_profile_replay", "mtp_reset", "mtp_destroy", "mtp_last_error", "mtp_strerror",
             "mtp_set_selection", "mtp_get_union_lattice", "mtp_set_sampling", "mtp_get_uniforms",
             "mtp_q_workspace_size", "mtp_q_count", "mtp_q_count_noalloc", "mtp_q_normalize",
-            "mtp_nar_prepare", "mtp_nar_run", "mtp_nar_get_codes", "mtp_nar_get_logits"]
+            "mtp_nar_prepare", "mtp_nar_run", "mtp_nar_get_codes", "mtp_nar_get_logits",
+            "mtp_pages_plan_workspace_size", "mtp_pages_plan", "mtp_pages_write", "mtp_pages_copy",
+            "mtp_pages_attention_workspace_size", "mtp_pages_attention",
+            "mtp_beam_select_workspace_size", "mtp_beam_select"]
 MTP_Q_COUNT_EOS = 1
 MTP_LATTICE_OWN, MTP_LATTICE_UNION = 0, 1
 MTP_SELECT_BEST, MTP_SELECT_SAMPLE = 0, 1
+MTP_ATTN_CAUSAL, MTP_ATTN_FULL = 0, 1
 
 
 class mtp_config(ctypes.Structure):
@@ -57,6 +61,45 @@ class mtp_sizes(ctypes.Structure):
 class mtp_buffers(ctypes.Structure):
     _fields_ = [("weights", ctypes.c_void_p), ("logq", ctypes.c_void_p),
                 ("kv_pool", ctypes.c_void_p), ("workspace", ctypes.c_void_p)]
+
+
+class mtp_cache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in (
+        "dtype", "num_pages", "n_kv_heads", "head_dim")]
+
+
+class mtp_plan_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_rows", "max_pages", "num_pages", "max_tokens")] + \
+               [(n, ctypes.c_void_p) for n in ("parent", "len", "add", "table_in", "table", "row_start", "kv_len",
+                                               "slots", "positions", "copies", "status", "workspace")] + \
+               [("workspace_bytes", ctypes.c_uint64)]
+
+
+class mtp_write_args(ctypes.Structure):
+    _fields_ = [("cache", mtp_cache), ("n_tokens", ctypes.c_int32), ("slots", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+class mtp_copy_args(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("page_bytes", ctypes.c_uint64), ("layer_stride", ctypes.c_uint64),
+                ("n_layers", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("n_copies", ctypes.c_int32),
+                ("copies", ctypes.c_void_p)]
+
+
+class mtp_attention_args(ctypes.Structure):
+    _fields_ = [("cache", mtp_cache)] + [(n, ctypes.c_int32) for n in (
+        "n_rows", "max_pages", "n_tokens", "n_heads", "mode", "window", "max_kv")] + [("scale", ctypes.c_float)] + \
+        [(n, ctypes.c_void_p) for n in ("table", "row_start", "kv_len", "q", "out")] + \
+        [("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("workspace", ctypes.c_void_p),
+         ("workspace_bytes", ctypes.c_uint64)]
+
+
+class mtp_beam_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_requests", "beams", "vocab", "eos_id", "eos_min")] + \
+               [("alpha", ctypes.c_float), ("logits", ctypes.c_void_p), ("ld", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("score", "len", "done", "out_score", "out_len", "out_done",
+                                               "out_parent", "out_token", "workspace")] + \
+               [("workspace_bytes", ctypes.c_uint64)]
 
 
 _P = ctypes.POINTER
@@ -89,6 +132,13 @@ _lib.mtp_nar_prepare.argtypes = [_ctx, ctypes.c_int, _i32p, _i32p, _i32p, _i32p,
 _lib.mtp_nar_run.argtypes = [_ctx]
 _lib.mtp_nar_get_codes.argtypes = [_ctx, _i32p]
 _lib.mtp_nar_get_logits.argtypes = [_ctx, ctypes.c_int, _f32p]
+for _n, _s in (("plan", mtp_plan_args), ("attention", mtp_attention_args)):
+    getattr(_lib, f"mtp_pages_{_n}_workspace_size").argtypes = [_P(_s), _P(ctypes.c_uint64)]
+    getattr(_lib, f"mtp_pages_{_n}").argtypes = [_P(_s), ctypes.c_void_p]
+_lib.mtp_pages_write.argtypes = [_P(mtp_write_args), ctypes.c_void_p]
+_lib.mtp_pages_copy.argtypes = [_P(mtp_copy_args), ctypes.c_void_p]
+_lib.mtp_beam_select_workspace_size.argtypes = [_P(mtp_beam_args), _P(ctypes.c_uint64)]
+_lib.mtp_beam_select.argtypes = [_P(mtp_beam_args), ctypes.c_void_p]
 _lib.mtp_get_seq_state.argtypes = [_ctx, _i32p, _i32p, _i32p, _i32p]
 _lib.mtp_get_tokens.argtypes = [_ctx, _i32p]
 _lib.mtp_profile_replay.argtypes = [_ctx, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_uint64,
@@ -323,6 +373,46 @@ def estimate_logq(tokens, offsets, vocab: int, eos_id: int, count_eos: bool, alp
     mtp_q_normalize(counts.data_ptr(), vocab, alpha, logq.data_ptr(), st.cuda_stream)
     ws.record_stream(st)
     return counts, logq, status
+
+
+# Paged serving: the argument structs of include/mtp.h (device pointers as
+# integers); serving.py fills them from torch tensors.
+def mtp_pages_plan_workspace_size(args: mtp_plan_args) -> int:
+    out = ctypes.c_uint64()
+    _check(_lib.mtp_pages_plan_workspace_size(args, out), None, "mtp_pages_plan_workspace_size")
+    return out.value
+
+
+def mtp_pages_plan(args: mtp_plan_args, stream: int) -> None:
+    _check(_lib.mtp_pages_plan(args, stream), None, "mtp_pages_plan")
+
+
+def mtp_pages_write(args: mtp_write_args, stream: int) -> None:
+    _check(_lib.mtp_pages_write(args, stream), None, "mtp_pages_write")
+
+
+def mtp_pages_copy(args: mtp_copy_args, stream: int) -> None:
+    _check(_lib.mtp_pages_copy(args, stream), None, "mtp_pages_copy")
+
+
+def mtp_pages_attention_workspace_size(args: mtp_attention_args) -> int:
+    out = ctypes.c_uint64()
+    _check(_lib.mtp_pages_attention_workspace_size(args, out), None, "mtp_pages_attention_workspace_size")
+    return out.value
+
+
+def mtp_pages_attention(args: mtp_attention_args, stream: int) -> None:
+    _check(_lib.mtp_pages_attention(args, stream), None, "mtp_pages_attention")
+
+
+def mtp_beam_select_workspace_size(args: mtp_beam_args) -> int:
+    out = ctypes.c_uint64()
+    _check(_lib.mtp_beam_select_workspace_size(args, out), None, "mtp_beam_select_workspace_size")
+    return out.value
+
+
+def mtp_beam_select(args: mtp_beam_args, stream: int) -> None:
+    _check(_lib.mtp_beam_select(args, stream), None, "mtp_beam_select")
 
 
 def mtp_reset(ctx) -> None:

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmtp.so")
 PROBE_LIB = os.path.join(PKG, "libmtp_probe.so")
 SOURCES = ["api.hip", "gemm.hip", "f32.hip", "gemv.hip", "attention.hip", "attn_mfma.hip", "rowops.hip", "select.hip", "qest.hip",
-           "qkv_attn.hip"]
+           "qkv_attn.hip", "pages.hip", "page_attn.hip", "beam.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

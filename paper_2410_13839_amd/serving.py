@@ -1,0 +1,218 @@
+"""Paged serving on torch tensors: block tables and slots from request
+lengths, cache writes, attention of new tokens over the cache, beam selection
+and the page copies of beams (include/mtp.h's mtp_pages_* and mtp_beam_*).
+
+Each function checks its tensors, allocates its outputs and workspace with
+torch and enqueues one library call on torch's current stream of the tensors'
+device; nothing is copied to the host and nothing waits, so the calls can be
+captured into a graph.  Tensors made on another stream must be ordered before
+the call by the caller, as for any torch operation.  A refused call raises
+ValueError (a tensor of the wrong kind) or MTPError (the library's own checks)
+with nothing launched.
+
+A step of a served batch:
+
+    plan = plan_pages(length, add, table, num_pages, max_tokens, parent=parents)
+    copy_pages(pools, plan.copies)                      # beams only
+    for l in range(layers):
+        write_pages(pools[l], plan.slots, k, v)
+        o = attend_pages(pools[l], plan.table, plan.row_start, plan.kv_len, q)
+    step = select_beams(logits, score, length, done, eos_id)
+
+A pool is [pages, 2, kv heads, 16 * head dim] in float32 or bfloat16 (pools of
+several layers: one more leading dimension), the page format of include/mtp.h.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding as _b
+
+PAGE = 16
+_DTYPE = {torch.float32: _b.MTP_DTYPE_F32, torch.bfloat16: _b.MTP_DTYPE_BF16}
+
+
+class PagePlan(NamedTuple):
+    """int32 tensors; the fields of mtp_plan_args."""
+    table: torch.Tensor       # [rows, max_pages]
+    row_start: torch.Tensor   # [rows + 1]
+    kv_len: torch.Tensor      # [rows]
+    slots: torch.Tensor       # [max_tokens]
+    positions: torch.Tensor   # [max_tokens]
+    copies: torch.Tensor      # [rows, 2]
+    status: torch.Tensor      # [4]: pages missing, bad rows, bad table entries, tokens without a slot
+
+
+class BeamStep(NamedTuple):
+    """[requests, beams] each; parent counts rows over all requests."""
+    score: torch.Tensor
+    length: torch.Tensor
+    done: torch.Tensor
+    parent: torch.Tensor
+    token: torch.Tensor
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(t: torch.Tensor, name: str, shape, device) -> int:
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _launch(fn, args, device) -> None:
+    """fn on torch's current stream of `device` (made the current device for the call)."""
+    if torch.cuda.current_device() == device.index:
+        fn(args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            fn(args, torch.cuda.current_stream().cuda_stream)
+
+
+def _device(t: torch.Tensor, name: str) -> torch.device:
+    if not t.is_cuda:
+        raise ValueError(f"{name}: a tensor on a GPU, not on {t.device}")
+    return t.device
+
+
+def _cache(pool: torch.Tensor) -> _b.mtp_cache:
+    if pool.dim() != 4 or pool.dtype not in _DTYPE or not pool.is_contiguous():
+        raise ValueError("pool: a contiguous float32 or bfloat16 tensor [pages, 2, kv heads, 16 * head dim]")
+    pages, two, heads, block = pool.shape
+    if two != 2 or block not in (PAGE * 64, PAGE * 128):
+        raise ValueError(f"pool: [pages, 2, kv heads, 16 * 64 or 16 * 128], not {tuple(pool.shape)}")
+    return _b.mtp_cache(pool.data_ptr(), _DTYPE[pool.dtype], pages, heads, block // PAGE)
+
+
+def _rows(t: torch.Tensor, name: str, pool: torch.Tensor, heads: Optional[int] = None) -> int:
+    """Token stride of [tokens, heads, head dim] rows in the pool's type."""
+    dim = pool.shape[3] // PAGE
+    if t.dtype != pool.dtype or t.device != pool.device or t.dim() != 3 or t.shape[2] != dim or \
+            (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name}: {pool.dtype} [tokens, {'heads' if heads is None else heads}, {dim}] on {pool.device}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.shape[0] and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim)):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+
+
+def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num_pages: int, max_tokens: int,
+               parent: Optional[torch.Tensor] = None, out_table: Optional[torch.Tensor] = None) -> PagePlan:
+    """Block tables, slots and positions of the next tokens (mtp_pages_plan).
+    length, add: int32 [rows]; table: int32 [rows, max_pages]; max_tokens: the
+    size of slots and positions (at least the new tokens' number).  out_table
+    receives the new table (a new tensor by default; `table` itself is allowed
+    without parents).  The status counts stay on the device."""
+    dev = _device(length, "length")
+    _need(table.dim() == 2 and length.dim() == 1, "length: [rows]; table: [rows, max_pages]")
+    n, m = table.shape
+    p_len, p_add = _ints(length, "length", (n,), dev), _ints(add, "add", (n,), dev)
+    p_in = _ints(table, "table", (n, m), dev)
+    p_par = None if parent is None else _ints(parent, "parent", (n,), dev)
+    i32 = torch.int32
+    new = torch.empty_like(table) if out_table is None else out_table
+    p_new = _ints(new, "out_table", (n, m), dev)
+    _need(p_par is None or p_new != p_in or n == 0, "out_table: not the table itself where rows have parents")
+    # one allocation for the small outputs: starts, lengths, copies, status
+    small = torch.empty(4 * n + 5, dtype=i32, device=dev)
+    tok = torch.empty((2, max_tokens), dtype=i32, device=dev)
+    base = small.data_ptr()
+    args = _b.mtp_plan_args(n, m, num_pages, max_tokens, p_par, p_len, p_add, p_in, p_new,
+                            base + 4 * 3 * n, base + 4 * 2 * n, tok.data_ptr() or None,
+                            tok.data_ptr() + 4 * max_tokens if max_tokens else None, base, base + 4 * (4 * n + 1), None, 0)
+    need = _b.mtp_pages_plan_workspace_size(args)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    if n == 0:
+        small.zero_()
+        tok.fill_(-1)
+    else:
+        _launch(_b.mtp_pages_plan, args, dev)
+    return PagePlan(new, small[3 * n:4 * n + 1], small[2 * n:3 * n], tok[0], tok[1], small[:2 * n].view(n, 2), small[4 * n + 1:])
+
+
+def write_pages(pool: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
+    """Stores k, v [tokens, kv heads, head dim] at `slots` int32 [tokens] of
+    one layer's pool (mtp_pages_write); slots outside the pool are skipped."""
+    dev = _device(pool, "pool")
+    cache = _cache(pool)
+    ks, vs = _rows(k, "k", pool, cache.n_kv_heads), _rows(v, "v", pool, cache.n_kv_heads)
+    _need(k.shape[0] == v.shape[0], "k and v: the same number of tokens")
+    p = _ints(slots, "slots", (k.shape[0],), dev)
+    _launch(_b.mtp_pages_write, _b.mtp_write_args(cache, k.shape[0], p, k.data_ptr(), v.data_ptr(), ks, vs), dev)
+
+
+def copy_pages(pools: torch.Tensor, copies: torch.Tensor) -> None:
+    """Copies the pages that a plan's `copies` names, in one layer's pool or,
+    with a leading dimension, in every layer's (mtp_pages_copy)."""
+    dev = _device(pools, "pools")
+    _need(pools.dim() in (4, 5) and pools.is_contiguous(), "pools: contiguous, [layers,] pages, 2, kv heads, 16 * head dim")
+    layers = pools.shape[0] if pools.dim() == 5 else 1
+    pages = pools.shape[-4]
+    page_bytes = pools.shape[-3] * pools.shape[-2] * pools.shape[-1] * pools.element_size()
+    _need(copies.dim() == 2, "copies: [n, 2]")
+    p = _ints(copies, "copies", (copies.shape[0], 2), dev)
+    _launch(_b.mtp_pages_copy, _b.mtp_copy_args(pools.data_ptr(), page_bytes, pages * page_bytes, layers, pages,
+                                                copies.shape[0], p), dev)
+
+
+def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor,
+                 q: torch.Tensor, causal: bool = True, window: int = 0, scale: Optional[float] = None, max_kv: int = 0,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [tokens, heads, head dim] over one layer's pool
+    (mtp_pages_attention): causal chunks (the queries are their rows' last
+    positions, `window` > 0 of them visible), or full attention with causal =
+    False.  scale defaults to head dim ** -0.5.  Tokens outside every row keep
+    what `out` holds (a new `out` starts undefined there)."""
+    dev = _device(pool, "pool")
+    cache = _cache(pool)
+    qs = _rows(q, "q", pool)
+    _need(table.dim() == 2, "table: [rows, max_pages]")
+    n, m = table.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    _need(out.shape == q.shape, "out: q's shape")
+    os = _rows(out, "out", pool)
+    args = _b.mtp_attention_args(cache, n, m, q.shape[0], q.shape[1], _b.MTP_ATTN_CAUSAL if causal else _b.MTP_ATTN_FULL,
+                                 window, max_kv, cache.head_dim ** -0.5 if scale is None else scale,
+                                 _ints(table, "table", (n, m), dev), _ints(row_start, "row_start", (n + 1,), dev),
+                                 _ints(kv_len, "kv_len", (n,), dev), q.data_ptr(), out.data_ptr(), qs, os, None, 0)
+    need = _b.mtp_pages_attention_workspace_size(args)
+    if need:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    _launch(_b.mtp_pages_attention, args, dev)
+    return out
+
+
+def select_beams(logits: torch.Tensor, score: torch.Tensor, length: torch.Tensor, done: torch.Tensor, eos_id: int,
+                 eos_min: int = 0, alpha: float = 0.0) -> BeamStep:
+    """The next beams of [requests, beams, vocab] float32 logits
+    (mtp_beam_select); score float32, length and done int32 [requests, beams].
+    Beams of one request that are still alike (at its start) are told apart by
+    a score of -infinity for all but the first."""
+    dev = _device(logits, "logits")
+    _need(logits.dim() == 3 and logits.dtype == torch.float32, "logits: float32 [requests, beams, vocab]")
+    r, w, v = logits.shape
+    ld = logits.stride(1) if w > 1 else (logits.stride(0) if r > 1 else v)
+    _need(v == 0 or logits.stride(2) == 1 or v == 1, "logits: a row's logits must be contiguous")
+    _need(r <= 1 or w <= 1 or logits.stride(0) == w * ld, "logits: the rows must be evenly spaced")
+    _need(score.dtype == torch.float32 and tuple(score.shape) == (r, w) and score.device == dev and score.is_contiguous(),
+          "score: contiguous float32 [requests, beams] on the logits' device")
+    new = torch.empty((5, r, w), dtype=torch.int32, device=dev)
+    base, step = new.data_ptr(), 4 * r * w
+    args = _b.mtp_beam_args(r, w, v, eos_id, eos_min, alpha, logits.data_ptr(), ld, score.data_ptr(),
+                            _ints(length, "length", (r, w), dev), _ints(done, "done", (r, w), dev), base, base + step,
+                            base + 2 * step, base + 3 * step, base + 4 * step, None, 0)
+    need = _b.mtp_beam_select_workspace_size(args)
+    if need:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    _launch(_b.mtp_beam_select, args, dev)
+    return BeamStep(new[0].view(torch.float32), new[1], new[2], new[3], new[4])
