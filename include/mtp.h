@@ -553,7 +553,8 @@ int mtp_pages_copy(const mtp_copy_args* args, void* hip_stream);
  * are right, only slower.  Scores, softmax and sums are float32; with a bf16
  * cache the probabilities are rounded to bf16 for the product with V.
  * 0 <= n_rows <= 4096, 1 <= max_pages <= 65536, 0 <= n_tokens < 2^24,
- * n_heads a multiple of n_kv_heads up to 1024, window >= 0, scale finite.
+ * n_heads a multiple of n_kv_heads up to 1024, (n_tokens + n_rows) * n_heads <
+ * 2^31, window >= 0 (0 with MTP_ATTN_FULL), scale finite.
  * q, out and the bytes of their strides are multiples of 16, the strides at
  * least n_heads * head_dim; out must not overlap another operand.  The
  * workspace is 256-byte aligned (NULL when the size call reports 0). */

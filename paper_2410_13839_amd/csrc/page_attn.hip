@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "../../include/mtp.h"
 #include "common.h"
 #include "wave.h"
@@ -22,61 +24,721 @@ namespace {
 constexpr int PG = 16;
 constexpr float LOG2E = 1.4426950408889634f;
 
-// The row whose tokens include t, or -1: the last c with row_start[c] <= t,
-// found by the whole wave (64 candidates a round).
-__device__ __forceinline__ int row_of_token(const mtp_attention_args& a, int t) {
-    int lo = 0, n = a.n_rows;                    // the answer lies in [lo, lo + n)
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
+// How a call is cut.  A tile is up to tt tokens of one row times the gs query
+// heads of one block (hb blocks make the group of a KV head): query row r of a
+// tile is token r / gs, head r % gs, so that grouped heads share the keys they
+// load.  Tiles are numbered row by row: row c owns the numbers row_start[c] /
+// tt + c up to the next row's first (at least as many as it needs; the others
+// are empty), so a workgroup finds its row by a search and the host needs no
+// lengths.  The keys of a tile are cut into n_splits runs of split_len, the
+// last one taking whatever is behind them; a tile with more than one live run
+// leaves partial sums for a second launch.
+struct AttnGeo {
+    int gs, hb, tt, n_tiles, n_splits, split_len;
+    float* acc;                // [n_tiles * heads * hb][n_splits][tile rows][D]
+    float2* ml;                // [...][tile rows] reference and sum
+};
+
+struct AttnTile {
+    int c, t0, nt;             // cache row, first token, tokens (0: empty)
+    int kv, pos0;              // the row's keys, the first token's position
+    int lo, hi;                // positions that some query of the tile sees
+};
+
+__device__ __forceinline__ int start_of(const mtp_attention_args& a, int c) {
+    return max(0, min(a.row_start[c], a.n_tokens));
+}
+
+// The tile's row, found by the whole wave, 64 candidates a round; uniform.
+__device__ __forceinline__ AttnTile find_tile(const mtp_attention_args& a, const AttnGeo& g, int tile) {
     const int lane = threadIdx.x & 63;
+    int lo = 0, n = a.n_rows;                    // the row lies in [lo, lo + n)
     while (n > 1) {
-        const int step = (n + 63) / 64;
-        const int i = lane * step;
-        const bool le = i < n && a.row_start[lo + i] <= t;
-        const int k = __popcll(__ballot(le));
-        if (k == 0) return -1;
+        const int step = (n + 63) >> 6, i = lane * step;
+        const bool le = i < n && start_of(a, lo + min(i, n - 1)) / g.tt + lo + i <= tile;
+        const int k = max(1, (int)__popcll(__ballot(le)));
         lo += (k - 1) * step;
         n = min(step, n - (k - 1) * step);
     }
-    return t >= a.row_start[lo] && t < a.row_start[lo + 1] ? lo : -1;
+    AttnTile t;
+    t.c = __builtin_amdgcn_readfirstlane(lo);
+    const int s = start_of(a, t.c), e = start_of(a, t.c + 1);
+    t.t0 = s + (tile - (s / g.tt + t.c)) * g.tt;
+    t.nt = max(0, min(g.tt, e - t.t0));
+    if (t.t0 < s) t.nt = 0;
+    t.kv = max(0, min(a.kv_len[t.c], PG * a.max_pages));
+    t.pos0 = t.kv - (e - s) + (t.t0 - s);
+    t.lo = 0;
+    t.hi = t.kv;
+    if (a.mode == MTP_ATTN_CAUSAL) {
+        t.hi = max(0, min(t.kv, t.pos0 + t.nt));
+        if (a.window > 0) t.lo = max(0, t.pos0 - a.window + 1);
+    }
+    return t;
 }
 
-// One wave per (token, head).
-template <typename T, int D>
-__global__ __launch_bounds__(64) void attn_simple_kernel(mtp_attention_args a) {
-    const int t = blockIdx.x, head = blockIdx.y, lane = threadIdx.x;
-    const int c = row_of_token(a, t);
-    if (c < 0) return;
-    const int s0 = max(a.row_start[c], 0), s1 = min(a.row_start[c + 1], a.n_tokens);
-    const int kv = max(0, min(a.kv_len[c], PG * a.max_pages));
-    const int pos = kv - (s1 - s0) + (t - s0);
-    int hi = kv, lo = 0;
+// The keys [k0, k1) of run `split`, and the number of live runs (at least 1;
+// a tile that sees nothing has one empty run).
+__device__ __forceinline__ int runs_of(const AttnGeo& g, const AttnTile& t, int split, int& k0, int& k1) {
+    const int base = t.lo & ~31;
+    const int live = min(g.n_splits, max(1, (t.hi - base + g.split_len - 1) / g.split_len));
+    k0 = base + split * g.split_len;
+    k1 = split == live - 1 ? t.hi : min(t.hi, k0 + g.split_len);
+    return live;
+}
+
+// What query row r of the tile sees: [lo, hi).
+__device__ __forceinline__ void sight_of(const mtp_attention_args& a, const AttnGeo& g, const AttnTile& t, int r, int& lo,
+                                         int& hi) {
+    lo = 0;
+    hi = t.kv;
     if (a.mode == MTP_ATTN_CAUSAL) {
-        hi = min(kv, pos + 1);
+        const int pos = t.pos0 + r / g.gs;
+        hi = min(t.kv, pos + 1);
         if (a.window > 0) lo = max(0, pos - a.window + 1);
     }
-    const int H = a.cache.n_kv_heads, hk = head / (a.n_heads / H);
-    const T* q = (const T*)a.q + (int64_t)t * a.q_stride + head * D;
-    const T* pool = (const T*)a.cache.pool;
-    float m = -INFINITY, l = 0.f, acc[D / 64] = {};
-    for (int j = lo; j < hi; ++j) {
-        const int pg = a.table[(size_t)c * a.max_pages + j / PG];
-        if (pg < 0 || pg >= a.cache.num_pages) continue;
-        const T* K = pool + ((size_t)pg * 2 * H + hk) * PG * D + (j % PG) * D;
-        const T* V = pool + ((size_t)pg * 2 * H + H + hk) * PG * D;
-        float s = 0.f;
-        for (int d = lane; d < D; d += 64) s += ActIO<T>::load(q + d) * ActIO<T>::load(K + d);
-        s = wave_sum64(s) * (a.scale * LOG2E);
-        const float mn = fmaxf(m, s);
-        const float r = m == -INFINITY ? 0.f : exp2f(m - mn), p = exp2f(s - mn);
-        m = mn;
-        l = l * r + p;
-        for (int i = 0; i < D / 64; ++i) {
-            const int d = lane + 64 * i;
-            acc[i] = acc[i] * r + p * ActIO<T>::load(V + (sizeof(T) == 2 ? d * PG + j % PG : (j % PG) * D + d));
+}
+
+__device__ __forceinline__ uint32_t pk2(float a, float b) { return bf16x2_bits(a, b); }
+
+// Two bf16 with those that are not finite set to zero; `seen` collects whether
+// there were any.
+__device__ __forceinline__ uint32_t finite2(uint32_t v, uint32_t& seen) {
+    const bool lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
+    seen |= (lo | hi) ? 1u : 0u;
+    return v & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+}
+
+// ------------------------------------------------------------ few query rows
+//
+// One workgroup per (tile of 16 query rows, KV head block, run of keys); its NW
+// waves take 32 keys (two pages) in turn, each with its own running maximum,
+// sum and output, merged through LDS once at the end.  Keys and values go
+// straight from the cache into the operands of the matrix products, the next
+// 32 keys' loads in flight while the current ones are used:
+//   S^T[key][q] = K[key][:] . Q[q][:]
+//   O^T[dim][q] += V^T[dim][key] P^T[key][q]
+// bf16: row 4 g + e of S's tile t (t = 0, 1) is key 8 g + 4 t + e of the 32, so
+// that lane (q, g) ends with the keys 8 g .. 8 g + 7, exactly its operand of
+// the second product, whose other operand is then one 16-byte load of the
+// transposed V block.  fp32 (16 keys a product): the contraction's index g of
+// step e is dimension 16 j + 4 g + e, or key 4 g + e, and row r of the output
+// tile dt is dimension (D / 16) r + dt, all 16-byte loads again.
+template <typename T, int D>
+struct Keys;                                     // 32 keys in operand order
+
+template <int D>
+struct Keys<bf16_t, D> {
+    uint4 k[2][D / 32];
+    uint4 v[D / 16];
+    __device__ __forceinline__ void load(const bf16_t* p0, const bf16_t* p1, size_t vofs, int r, int g) {
+        // r >= 8: the second page's keys; g >= 2 likewise for V
+        const bf16_t* kp = (r & 8 ? p1 : p0) + (8 * ((r >> 2) & 1) + (r & 3)) * D + 8 * g;
+        const bf16_t* vp = (g & 2 ? p1 : p0) + vofs + r * PG + 8 * (g & 1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) k[t][j] = *reinterpret_cast<const uint4*>(kp + 4 * t * D + 32 * j);
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) v[dt] = *reinterpret_cast<const uint4*>(vp + 16 * dt * PG);
+    }
+};
+template <int D>
+struct Keys<float, D> {
+    float4 k[2][D / 16];
+    float4 v[2][4][D / 64];
+    __device__ __forceinline__ void load(const float* p0, const float* p1, size_t vofs, int r, int g) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const float* kp = (t ? p1 : p0) + r * D + 4 * g;
+            const float* vp = (t ? p1 : p0) + vofs + 4 * g * D + (D / 16) * r;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) k[t][j] = *reinterpret_cast<const float4*>(kp + 16 * j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) v[t][e][i] = *reinterpret_cast<const float4*>(vp + e * D + 4 * i);
         }
     }
-    T* o = (T*)a.out + (int64_t)t * a.out_stride + head * D;
-    const float inv = l > 0.f ? 1.f / l : (m == -INFINITY ? 0.f : NAN);
-    for (int i = 0; i < D / 64; ++i) ActIO<T>::store(o + lane + 64 * i, acc[i] * inv);
+};
+
+// Output dimension of accumulator (dt, e) of lane group g.
+template <typename T, int D>
+__device__ __forceinline__ int dim_of(int dt, int g, int e) {
+    return sizeof(T) == 2 ? 16 * dt + 4 * g + e : (D / 16) * (4 * g + e) + dt;
+}
+
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_args a, AttnGeo g) {
+    constexpr int QR = 16, ND = D / 16;
+    extern __shared__ __attribute__((aligned(16))) float s_acc[];    // [NW][16][D], dimensions in order
+    __shared__ float s_m[NW][QR], s_l[NW][QR];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, gr = lane >> 4;
+    const int H = a.cache.n_kv_heads, HB = H * g.hb;
+    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb;
+    const AttnTile t = find_tile(a, g, tile);
+    if (t.nt == 0) return;
+    int k0, k1;
+    const int live = runs_of(g, t, blockIdx.y, k0, k1);
+    if ((int)blockIdx.y >= live) return;
+
+    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs;      // first head of the block in its group
+    const int heads = min(g.gs, group - h0), rows = t.nt * g.gs;
+    const int rc = r < rows && r % g.gs < heads ? r : 0;                  // rows that do not exist compute row 0
+    const T* qp = (const T*)a.q + (int64_t)(t.t0 + rc / g.gs) * a.q_stride + (hk * group + h0 + rc % g.gs) * D;
+    uint4 q[sizeof(T) == 2 ? D / 32 : D / 16];
+#pragma unroll
+    for (int j = 0; j < (sizeof(T) == 2 ? D / 32 : D / 16); ++j)
+        q[j] = *reinterpret_cast<const uint4*>(qp + (sizeof(T) == 2 ? 32 * j + 8 * gr : 16 * j + 4 * gr));
+    int rlo, rhi;
+    sight_of(a, g, t, rc, rlo, rhi);
+    // keys that every query of the tile sees: [alo, ahi)
+    int alo, ahi, unused;
+    sight_of(a, g, t, rows - 1, alo, unused);
+    sight_of(a, g, t, 0, unused, ahi);
+
+    const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
+    const T* pool = (const T*)a.cache.pool + (size_t)hk * PG * D;
+    const int32_t* tab = a.table + (size_t)t.c * a.max_pages;
+    const int npairs = (k1 - k0 + 31) >> 5;                              // of the run
+    const int mine = npairs > wave ? (npairs - wave + NW - 1) / NW : 0;  // of this wave: wave, wave + NW, ...
+    // lane i: the pages of this wave's pair i (64 at a time); -1 where there is none
+    int pg0 = -1, pg1 = -1;
+    auto pages = [&](int i) {
+        const int p = (k0 >> 4) + 2 * (wave + NW * (i + lane));
+        int x = -1, y = -1;
+        if (i + lane < mine) {
+            x = p < a.max_pages ? tab[p] : -1;
+            y = p + 1 < a.max_pages ? tab[p + 1] : -1;
+        }
+        pg0 = x >= 0 && x < a.cache.num_pages ? x : -1;
+        pg1 = y >= 0 && y < a.cache.num_pages ? y : -1;
+    };
+    // (fp32 keys of 128 dimensions: 128 registers a set, one set only)
+    constexpr int PD = sizeof(T) * D > 256 ? 1 : 2;
+    Keys<T, D> kv[PD];
+    int bad[PD] = {};                                                     // bit 0, 1: the pair's page is not there
+    auto fetch = [&](Keys<T, D>& x, int& b, int i) {
+        if ((i & 63) == 0) pages(i);
+        const int x0 = __builtin_amdgcn_readlane(pg0, i & 63), x1 = __builtin_amdgcn_readlane(pg1, i & 63);
+        b = (x0 < 0 ? 1 : 0) | (x1 < 0 ? 2 : 0);
+        x.load(pool + (size_t)max(x0, 0) * pstr, pool + (size_t)max(x1, 0) * pstr, vofs, r, gr);
+    };
+
+    const float c = a.scale * LOG2E;
+    float m = -INFINITY, l = 0.f;
+    f32x4_t o[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+    auto use = [&](Keys<T, D>& x, int b, int i) {
+        const int kb = k0 + 32 * (wave + NW * i);
+        // s[u]: bf16, keys kb + 8 gr + u; fp32, keys kb + 16 (u / 4) + 4 gr + u % 4
+        float s[8];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.k[tt][j]),
+                                                                  __builtin_bit_cast(bf16x8_t, q[j]), acc, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    const float4 kk = x.k[tt][j], qq = __builtin_bit_cast(float4, q[j]);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kk.x, qq.x, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kk.y, qq.y, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kk.z, qq.z, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kk.w, qq.w, acc, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * tt + e] = acc[e] * c;
+        }
+        auto key_of = [&](int u) { return kb + (sizeof(T) == 2 ? 8 * gr + u : 16 * (u >> 2) + 4 * gr + (u & 3)); };
+        auto there = [&](int u) {                                        // the key's page is in the pool
+            return sizeof(T) == 2 ? !(b >> (gr >> 1) & 1) : !(b >> (u >> 2) & 1);
+        };
+        const bool edge = kb < alo || kb + 32 > ahi || kb + 32 > k1 || b;    // uniform
+        uint32_t odd = 0;
+        if (edge) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int key = key_of(u);
+                s[u] = key >= rlo && key < rhi && key < k1 && there(u) ? s[u] : -INFINITY;
+            }
+            // values that no query sees are not multiplied (0 x infinity, 0 x NaN); among those that some see and
+            // some do not, the ones that are not finite are taken out here and added below
+            if constexpr (sizeof(T) == 2) {
+                uint32_t in[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int y0 = kb + 8 * gr + 2 * j, y1 = y0 + 1;
+                    in[j] = there(0) ? (y0 >= t.lo && y0 < k1 ? 0xffffu : 0u) | (y1 >= t.lo && y1 < k1 ? 0xffff0000u : 0u) : 0u;
+                }
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) {
+                    uint4& v = x.v[dt];
+                    v = make_uint4(finite2(v.x & in[0], odd), finite2(v.y & in[1], odd), finite2(v.z & in[2], odd),
+                                   finite2(v.w & in[3], odd));
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int key = key_of(u);
+                    const bool in = key >= t.lo && key < k1 && there(u);
+#pragma unroll
+                    for (int i2 = 0; i2 < D / 64; ++i2) {
+                        float* v = reinterpret_cast<float*>(&x.v[u >> 2][u & 3][i2]);
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) {
+                            const bool fin = fabsf(v[d]) < INFINITY;
+                            odd |= in && !fin ? 1u : 0u;
+                            v[d] = in && fin ? v[d] : 0.f;
+                        }
+                    }
+                }
+            }
+        }
+        float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+        mx = xor16_max(mx);
+        mx = xor32_max(mx);
+        if (__any(mx > m)) {
+            const float mn = fmaxf(m, mx), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
+        }
+        const float mm = m == -INFINITY ? 0.f : m;
+        float p[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) p[u] = __builtin_amdgcn_exp2f(s[u] - mm);
+        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        if constexpr (sizeof(T) == 2) {
+            const bf16x8_t pf = __builtin_bit_cast(
+                bf16x8_t, make_uint4(pk2(p[0], p[1]), pk2(p[2], p[3]), pk2(p[4], p[5]), pk2(p[6], p[7])));
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.v[dt]), pf, o[dt], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                        reinterpret_cast<const float*>(&x.v[u >> 2][u & 3][0])[dt], p[u], o[dt], 0, 0, 0);
+        }
+        if (__any(odd)) {
+            // an infinite or NaN value reaches exactly the queries that see it
+            const int pr = wave + NW * i;
+            for (int u = 0; u < 32; ++u) {
+                const int key = kb + u, at = (k0 >> 4) + 2 * pr + (u >> 4);
+                if (key >= k1 || key < t.lo || (b >> (u >> 4) & 1)) continue;
+                const T* vb = pool + (size_t)tab[at] * pstr + vofs;
+                const bool sees = key >= rlo && key < rhi;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int d = dim_of<T, D>(dt, gr, e);
+                        const float v = ActIO<T>::load(vb + (sizeof(T) == 2 ? d * PG + (u & 15) : (u & 15) * D + d));
+                        if (sees && !(fabsf(v) < INFINITY)) o[dt][e] += v;
+                    }
+            }
+        }
+    };
+
+    if constexpr (PD == 1) {
+        for (int i = 0; i < mine; ++i) {
+            fetch(kv[0], bad[0], i);
+            use(kv[0], bad[0], i);
+        }
+    } else {
+        if (mine > 0) fetch(kv[0], bad[0], 0);
+        for (int i = 0; i < mine; i += 2) {
+            if (i + 1 < mine) fetch(kv[1], bad[1], i + 1);
+            use(kv[0], bad[0], i);
+            if (i + 1 < mine) {
+                if (i + 2 < mine) fetch(kv[0], bad[0], i + 2);
+                use(kv[1], bad[1], i + 1);
+            }
+        }
+    }
+    l = xor16_sum(l);
+    l = xor32_sum(l);
+
+    // merge the waves
+    if (gr == 0) { s_m[wave][r] = m; s_l[wave][r] = l; }
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) {
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<f32x4_t*>(&s_acc[(wave * QR + r) * D + 16 * dt + 4 * gr]) = o[dt];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_acc[(wave * QR + r) * D + dim_of<T, D>(dt, gr, e)] = o[dt][e];
+        }
+    }
+    __syncthreads();
+    const size_t slot = ((size_t)blockIdx.x * g.n_splits + blockIdx.y) * QR;
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * NW) {
+        const int qr = i / (D / 4), d = (i - qr * (D / 4)) * 4;
+        if (qr % g.gs >= heads) continue;
+        float mm = s_m[0][qr];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) mm = fmaxf(mm, s_m[w][qr]);
+        float ll = 0.f;
+        f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = s_m[w][qr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][qr] - mm);
+            ll += f * s_l[w][qr];
+            const f32x4_t ow = *reinterpret_cast<const f32x4_t*>(&s_acc[(w * QR + qr) * D + d]);
+            if (s_m[w][qr] != -INFINITY) v += ow * f;
+        }
+        if (live > 1) {
+            *reinterpret_cast<f32x4_t*>(&g.acc[(slot + qr) * D + d]) = v;
+            if (d == 0) g.ml[slot + qr] = make_float2(mm, ll);
+        } else {
+            // (a row that sees nothing has a sum of 0; one whose scores are not numbers keeps that)
+            const float inv = ll == 0.f ? 0.f : 1.f / ll;
+            T* op = (T*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + d;
+            if constexpr (sizeof(T) == 2)
+                *reinterpret_cast<uint2*>(op) = make_uint2(pk2(v[0] * inv, v[1] * inv), pk2(v[2] * inv, v[3] * inv));
+            else
+                *reinterpret_cast<f32x4_t*>(op) = v * inv;
+        }
+    }
+}
+
+// ----------------------------------------------------------- many query rows
+//
+// One workgroup per (tile of 128 query rows, KV head block, run of keys) for
+// bf16 caches: four waves of 32 query rows each over blocks of 64 keys (four
+// pages) that they share through LDS, the next block's loads going straight to
+// LDS while the current one is used.
+//   S^T[key][q] = K[key][:] . Q[q][:]       32 x 32 x 16 products
+//   O^T[dim][q] += V^T[dim][key] P^T[key][q]
+// Row 16 s + 8 j + 4 h + e of a 32-key tile of S is key 16 s + 8 h + 4 j + e, so
+// that lane (q, h) holds the keys 16 s + 8 h .. + 7 in its registers 8 s .. 8 s
+// + 7: its operand of the second product, the other one being 16 bytes of a V
+// page.  In LDS a page's V block is as in the cache (a wave's operand reads are
+// 1 KB in a row); K rows are whole multiples of the banks, so the 16-byte
+// pieces of a row are stored in an order that its slot shifts (the address that
+// a lane loads from, not where it stores).
+// The reference m moves only when a score exceeds it by 8 (float32 sums and
+// bf16 probabilities up to 2^8 keep their relative precision).
+constexpr int TR = 128;                          // query rows of a tile
+constexpr int KB = 64;                           // keys of a block
+
+typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a, AttnGeo g) {
+    constexpr float MSTEP = 8.0f;
+    constexpr int CW = D / 8;                    // 16-byte pieces of a K row
+    __shared__ __attribute__((aligned(1024))) bf16_t s_k[2][KB * D], s_v[2][KB * D];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qc = lane & 31, hh = lane >> 5;
+    const int H = a.cache.n_kv_heads, HB = H * g.hb;
+    // the tiles of one head and run on one XCD (workgroups are dealt to the 8 XCDs in turn), whose L2 then holds
+    // their keys
+    const unsigned total = (unsigned)g.n_tiles * HB * g.n_splits, chunk = (total + 7) / 8;
+    const unsigned wi = (blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= chunk || wi >= total) return;
+    const int tile = wi % g.n_tiles, hs = wi / g.n_tiles, split = hs % g.n_splits, hbi = hs / g.n_splits, hk = hbi / g.hb;
+    const AttnTile t = find_tile(a, g, tile);
+    if (t.nt == 0) return;
+    int k0, k1;
+    const int live = runs_of(g, t, split, k0, k1);
+    if (split >= live) return;
+
+    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs;
+    const int heads = min(g.gs, group - h0), rows = t.nt * g.gs;
+    const bool wave_on = 32 * wave < rows;       // uniform
+    const int r0 = min(32 * wave, rows - 1), r1 = min(32 * wave + 31, rows - 1);
+    const int row = min(32 * wave + qc, r1);
+    const int hq = row % g.gs < heads ? row % g.gs : 0;   // heads that do not exist compute the block's first
+    const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(t.t0 + row / g.gs) * a.q_stride + (hk * group + h0 + hq) * D + 8 * hh;
+    // scores are S x c with c > 0: a negative scale turns the queries' signs, scale 0 their values to 0
+    const float c = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
+    bf16x8_t q[D / 16];
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+        u32x4_t v = *reinterpret_cast<const u32x4_t*>(qp + 16 * j);
+        if (a.scale < 0.f) v ^= 0x80008000u;
+        if (a.scale == 0.f) v = u32x4_t{0, 0, 0, 0};
+        q[j] = __builtin_bit_cast(bf16x8_t, v);
+    }
+    int rlo, rhi, wlo, whi, alo, ahi;            // what this lane's row sees; some row of the wave; every row of it
+    sight_of(a, g, t, row, rlo, rhi);
+    sight_of(a, g, t, r0, wlo, ahi);
+    sight_of(a, g, t, r1, alo, whi);
+
+    const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
+    const bf16_t* pool = (const bf16_t*)a.cache.pool + (size_t)hk * PG * D;
+    const int32_t* tab = a.table + (size_t)t.c * a.max_pages;
+    const int nb = k1 > k0 ? (k1 - k0 + KB - 1) / KB : 0;
+    const int pg_end = min(a.max_pages, (k1 + PG - 1) / PG);
+    // lane i: page i of the next 64 (16 blocks), -1 where there is none
+    auto pages = [&](int blk) {
+        const int p = k0 / PG + 4 * blk + lane;
+        const int x = p < pg_end ? tab[p] : -1;
+        return x >= 0 && x < a.cache.num_pages ? x : -1;
+    };
+    int pg_now = pages(0), pg_next = pages(16);
+    // what each lane loads of a page in one step: K's piece of slot `slot`, V's in order
+    constexpr int SPP = D / 32;                  // wave steps (1 KB) per page block
+    auto stage = [&](int buf, int blk) {
+        if ((blk & 15) == 0 && blk > 0) { pg_now = pg_next; pg_next = pages(blk + 16); }
+        int bad = 0;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            bad |= __builtin_amdgcn_readlane(pg_now, 4 * (blk & 15) + p) < 0 ? 1 << p : 0;
+#pragma unroll
+        for (int i = 0; i < SPP; ++i) {
+            const int step = 4 * i + wave, p = step / SPP, in = (step % SPP) * 64 + lane;
+            const int pg = max(__builtin_amdgcn_readlane(pg_now, 4 * (blk & 15) + p), 0);
+            const bf16_t* base = pool + (size_t)pg * pstr;
+            const int slot = in / CW, piece = (in % CW) ^ (D == 128 ? slot : (slot >> 1) & 7);
+            __builtin_amdgcn_global_load_lds((gptr_t)(base + slot * D + piece * 8), (lptr_t)(&s_k[buf][step * 512]), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr_t)(base + vofs + in * 8), (lptr_t)(&s_v[buf][step * 512]), 16, 0, 0);
+        }
+        return bad;
+    };
+
+    float m = -INFINITY, l = 0.f;
+    f32x16_t o[D / 32];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+
+    // K operand: row qc of a tile is key krow
+    const int krow = (qc & 16) | ((qc & 4) << 1) | ((qc & 8) >> 1) | (qc & 3);
+    const int ksw = D == 128 ? krow & 15 : (krow >> 1) & 7;
+
+    auto use = [&](int buf, int kb, int bad) {
+        const bf16_t* K = s_k[buf] + krow * D;
+        const bf16_t* V = s_v[buf] + qc * PG + 8 * hh;
+        f32x16_t s[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    *reinterpret_cast<const bf16x8_t*>(K + 32 * tt * D + ((2 * j + hh) ^ ksw) * 8), q[j], s[tt], 0, 0, 0);
+        }
+        // register i of tile tt: key kb + 32 tt + 16 (i / 8) + 8 hh + i % 8, page 2 tt + i / 8 of the block
+        const bool edge = kb < alo || kb + KB > ahi || kb + KB > k1 || bad;   // uniform over the wave
+        if (edge) {
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = kb + 32 * tt + 16 * (i >> 3) + 8 * hh + (i & 7);
+                    const bool ok = key >= rlo && key < rhi && key < k1 && !(bad >> (2 * tt + (i >> 3)) & 1);
+                    s[tt][i] = ok ? s[tt][i] : -INFINITY;
+                }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[tt][i]);
+        mx *= c;
+        if (__any(mx > (m == -INFINITY ? -INFINITY : m + MSTEP))) {
+            mx = xor32_max(mx);
+            const float mn = fmaxf(m, mx), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) o[dt] *= f;
+        }
+        const float mm = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+        bf16x8_t p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + i], c, -mm));
+            sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+            p[u] = __builtin_bit_cast(bf16x8_t, make_uint4(pk2(e[0], e[1]), pk2(e[2], e[3]), pk2(e[4], e[5]), pk2(e[6], e[7])));
+        }
+        l += sum;
+        if (!edge) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        *reinterpret_cast<const bf16x8_t*>(V + u * PG * D + 32 * dt * PG), p[u], o[dt], 0, 0, 0);
+            return;
+        }
+        // values that no query sees are not multiplied (0 x infinity, 0 x NaN); among those that some see and some
+        // do not, the ones that are not finite are taken out here and added below
+        uint32_t odd = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            uint32_t in[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int y0 = kb + 16 * u + 8 * hh + 2 * j, y1 = y0 + 1;
+                in[j] = bad >> u & 1 ? 0u
+                                     : (y0 >= t.lo && y0 < k1 ? 0xffffu : 0u) | (y1 >= t.lo && y1 < k1 ? 0xffff0000u : 0u);
+            }
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) {
+                uint4 v = *reinterpret_cast<const uint4*>(V + u * PG * D + 32 * dt * PG);
+                v = make_uint4(finite2(v.x & in[0], odd), finite2(v.y & in[1], odd), finite2(v.z & in[2], odd),
+                               finite2(v.w & in[3], odd));
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[u], o[dt], 0, 0, 0);
+            }
+        }
+        if (__any(odd)) {
+            // an infinite or NaN value reaches exactly the queries that see it
+            for (int u = 0; u < KB; ++u) {
+                const int key = kb + u;
+                if (key >= k1 || key < t.lo || (bad >> (u >> 4) & 1)) continue;
+                const bool sees = key >= rlo && key < rhi;
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int d = 32 * dt + 8 * (i >> 2) + 4 * hh + (i & 3);
+                        const float v = bf16_to_f32(s_v[buf][(u >> 4) * PG * D + d * PG + (u & 15)]);
+                        if (sees && !(fabsf(v) < INFINITY)) o[dt][i] += v;
+                    }
+            }
+        }
+    };
+
+    int bad = nb > 0 ? stage(0, 0) : 0;
+    for (int j = 0; j < nb; ++j) {
+        // this wave's loads of block j have landed; all waves' have, and all are done with block j - 1's buffer
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int now = bad, kb = k0 + KB * j;
+        if (j + 1 < nb) bad = stage((j + 1) & 1, j + 1);
+        if (wave_on && kb < whi && kb + KB > wlo) use(j & 1, kb, now);
+    }
+    l = xor32_sum(l);
+
+    const int qr = 32 * wave + qc;
+    if (qr >= rows || qr % g.gs >= heads) return;
+    // register i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 hh + i % 4
+    if (live > 1) {
+        const size_t slot = (((size_t)tile * HB + hbi) * g.n_splits + split) * TR + qr;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4_t*>(&g.acc[slot * D + 32 * dt + 2 * i + 4 * hh]) =
+                    f32x4_t{o[dt][i], o[dt][i + 1], o[dt][i + 2], o[dt][i + 3]};
+        if (hh == 0) g.ml[slot] = make_float2(m, l);
+    } else {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16_t* op = (bf16_t*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + 4 * hh;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<uint2*>(op + 32 * dt + 2 * i) =
+                    make_uint2(pk2(o[dt][i] * inv, o[dt][i + 1] * inv), pk2(o[dt][i + 2] * inv, o[dt][i + 3] * inv));
+    }
+}
+
+// Joins a tile's runs: one workgroup per (tile, head block), RT rows a tile.
+template <typename T, int D, int RT>
+__global__ __launch_bounds__(256) void attn_join_kernel(mtp_attention_args a, AttnGeo g) {
+    const int H = a.cache.n_kv_heads, HB = H * g.hb;
+    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb;
+    const AttnTile t = find_tile(a, g, tile);
+    if (t.nt == 0) return;
+    int k0, k1;
+    const int live = runs_of(g, t, 0, k0, k1);
+    if (live <= 1) return;
+    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs, heads = min(g.gs, group - h0), rows = t.nt * g.gs;
+    const size_t slot = (size_t)blockIdx.x * g.n_splits * RT;
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
+        const int qr = i / (D / 4), d = (i - qr * (D / 4)) * 4;
+        if (qr % g.gs >= heads) continue;
+        float m = -INFINITY, l = 0.f;
+        f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < live; ++s) {
+            const float2 x = g.ml[slot + (size_t)s * RT + qr];
+            if (x.x == -INFINITY && x.y == 0.f) continue;
+            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(&g.acc[(slot + (size_t)s * RT + qr) * D + d]);
+            const float mn = fmaxf(m, x.x);
+            const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+            const float f1 = x.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x.x - mn);
+            l = l * f0 + x.y * f1;
+            v = (m == -INFINITY ? f32x4_t{0.f, 0.f, 0.f, 0.f} : v * f0) + w * f1;
+            m = mn;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T* op = (T*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + d;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<uint2*>(op) = make_uint2(pk2(v[0] * inv, v[1] * inv), pk2(v[2] * inv, v[3] * inv));
+        else
+            *reinterpret_cast<f32x4_t*>(op) = v * inv;
+    }
+}
+
+// ------------------------------------------------------------------- launches
+template <typename T, int D, int NW>
+int rows_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
+    const size_t lds = (size_t)NW * 16 * D * 4;
+    const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
+    if (lds > 64 * 1024 &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_rows_kernel<T, D, NW>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        return MTP_EHIP;
+    hipLaunchKernelGGL((attn_rows_kernel<T, D, NW>), dim3(work, g.n_splits), dim3(64 * NW), lds, st, a, g);
+    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<T, D, 16>), dim3(work), dim3(256), 0, st, a, g);
+    return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
+}
+
+template <int D>
+int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
+    const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
+    hipLaunchKernelGGL((attn_tile_kernel<D>), dim3((work * g.n_splits + 7) / 8 * 8), dim3(256), 0, st, a, g);
+    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<bf16_t, D, TR>), dim3(work), dim3(256), 0, st, a, g);
+    return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
+}
+
+// The cut of a call: kernel, tile shape, runs and the workspace of the partial
+// sums.
+struct AttnCut { AttnGeo g; bool wide; uint64_t acc_bytes, bytes; };
+
+AttnCut attn_cut(const mtp_attention_args& a) {
+    AttnCut x{};
+    const int group = a.n_heads / a.cache.n_kv_heads;
+    x.g.hb = (group + 15) / 16;
+    x.g.gs = (group + x.g.hb - 1) / x.g.hb;
+    const int64_t kv_all = (int64_t)PG * a.max_pages, kv = a.max_kv > 0 && a.max_kv < kv_all ? a.max_kv : kv_all;
+    x.wide = a.cache.dtype == MTP_DTYPE_BF16 && (int64_t)a.n_tokens * x.g.gs > 32ll * a.n_rows;
+    const int rt = x.wide ? TR : 16, key_min = x.wide ? 512 : 256;
+    x.g.tt = rt / x.g.gs;
+    x.g.n_tiles = a.n_tokens / x.g.tt + a.n_rows;
+    const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
+    int64_t n = std::min<int64_t>((512 + work - 1) / work, kv / key_min);
+    n = std::max<int64_t>(1, std::min<int64_t>(n, 256));
+    x.g.n_splits = (int)n;
+    x.g.split_len = (int)(((kv + n - 1) / n + KB - 1) / KB * KB);
+    if (n > 1) {
+        x.acc_bytes = (uint64_t)work * n * rt * a.cache.head_dim * 4;
+        x.bytes = x.acc_bytes + (uint64_t)work * n * rt * 8;
+    }
+    return x;
 }
 
 bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }
@@ -88,8 +750,10 @@ int attn_check(const mtp_attention_args* a) {
     if (a->n_rows < 0 || a->n_rows > 4096 || a->max_pages < 1 || a->max_pages > 65536 || a->n_tokens < 0 ||
         a->n_tokens >= (1 << 24) || a->n_heads < 1 || a->n_heads > 1024 || a->n_heads % a->cache.n_kv_heads)
         return MTP_EINVAL;
+    if ((int64_t)(a->n_tokens + a->n_rows) * a->n_heads >= (1ll << 31)) return MTP_EINVAL;
     if (a->mode != MTP_ATTN_CAUSAL && a->mode != MTP_ATTN_FULL) return MTP_EINVAL;
-    if (a->window < 0 || (a->mode == MTP_ATTN_FULL && a->window != 0) || a->max_kv < 0 || !isfinite(a->scale)) return MTP_EINVAL;
+    if (a->window < 0 || (a->mode == MTP_ATTN_FULL && a->window != 0) || a->max_kv < 0 || !isfinite(a->scale * LOG2E))
+        return MTP_EINVAL;
     return MTP_OK;
 }
 
@@ -101,7 +765,7 @@ extern "C" {
 int mtp_pages_attention_workspace_size(const mtp_attention_args* args, uint64_t* bytes) {
     const int rc = mtp::attn_check(args);
     if (rc != MTP_OK || !bytes) return MTP_EINVAL;
-    *bytes = 0;
+    *bytes = mtp::attn_cut(*args).bytes;
     return MTP_OK;
 }
 
@@ -115,16 +779,18 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream) {
     if (!aligned(a.table, 4) || !aligned(a.row_start, 4) || !aligned(a.kv_len, 4) || !aligned(a.q, 16) ||
         !aligned(a.out, 16) || a.q_stride < row || a.out_stride < row || a.q_stride % per || a.out_stride % per)
         return MTP_EINVAL;
-    const dim3 grid(a.n_tokens, a.n_heads), block(64);
-    hipStream_t st = (hipStream_t)hip_stream;
-    if (a.cache.dtype == MTP_DTYPE_BF16) {
-        if (a.cache.head_dim == 64) hipLaunchKernelGGL((attn_simple_kernel<bf16_t, 64>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((attn_simple_kernel<bf16_t, 128>), grid, block, 0, st, a);
-    } else {
-        if (a.cache.head_dim == 64) hipLaunchKernelGGL((attn_simple_kernel<float, 64>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((attn_simple_kernel<float, 128>), grid, block, 0, st, a);
+    AttnCut x = attn_cut(a);
+    if (x.bytes) {
+        if (!aligned(a.workspace, 256)) return MTP_EINVAL;
+        if (a.workspace_bytes < x.bytes) return MTP_ENOMEM;
+        x.g.acc = (float*)a.workspace;
+        x.g.ml = (float2*)((char*)a.workspace + x.acc_bytes);
     }
-    return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool bf = a.cache.dtype == MTP_DTYPE_BF16;
+    if (x.wide) return a.cache.head_dim == 64 ? tile_go<64>(st, a, x.g) : tile_go<128>(st, a, x.g);
+    if (a.cache.head_dim == 64) return bf ? rows_go<bf16_t, 64, 4>(st, a, x.g) : rows_go<float, 64, 4>(st, a, x.g);
+    return bf ? rows_go<bf16_t, 128, 4>(st, a, x.g) : rows_go<float, 128, 4>(st, a, x.g);
 }
 
 }  // extern "C"

@@ -116,7 +116,7 @@ def test_copy_refuses(kw):
 
 @pytest.mark.parametrize("kw", [dict(n_rows=-1), dict(n_rows=4097), dict(max_pages=0), dict(max_pages=65537),
                                 dict(n_tokens=-1), dict(n_tokens=1 << 24), dict(n_heads=0), dict(n_heads=6),
-                                dict(n_heads=1028), dict(mode=2), dict(mode=-1), dict(window=-1), dict(mode=1, window=5),
+                                dict(n_heads=1028), dict(n_heads=1024, n_tokens=1 << 22, q_stride=1 << 16, out_stride=1 << 16), dict(mode=2), dict(mode=-1), dict(window=-1), dict(mode=1, window=5),
                                 dict(max_kv=-1), dict(scale=INF), dict(scale=NAN), dict(table=0), dict(table=258),
                                 dict(row_start=0), dict(kv_len=0), dict(q=0), dict(q=1032), dict(out=0), dict(out=2056),
                                 dict(q_stride=504), dict(q_stride=516), dict(out_stride=511)])
