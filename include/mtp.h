@@ -482,7 +482,8 @@ typedef struct mtp_cache {
  * every other pair of arrays must be disjoint.  0 <= n_rows <= 4096,
  * 1 <= max_pages <= 65536, 1 <= num_pages < 2^27, 0 <= max_tokens < 2^31;
  * len[p] + add[c] <= 16 * max_pages.  Arrays are 4-byte aligned, the
- * workspace (about num_pages / 8 + 16 n_rows bytes) 256-byte. */
+ * workspace (about num_pages / 8 + 16 n_rows bytes; none, and NULL, when the
+ * size call reports 0) 256-byte. */
 typedef struct mtp_plan_args {
     int32_t n_rows, max_pages, num_pages, max_tokens;
     const int32_t* parent;      /* [n_rows], or NULL                           */
@@ -589,13 +590,13 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream);
  * does a candidate whose score is NaN or +infinity; candidates of -infinity
  * come last.
  * Scores and ranks are formed in float64 from float32 exponentials summed in
- * float64, a beam's own candidates ordered by their logits.  Written per next
+ * float64; a beam's own candidates are ordered by their logits.  Written per next
  * beam: out_score (float32), out_len, out_done (done before, or the token is
  * eos_id), out_parent (the row w it continues, as mtp_pages_plan's parent) and
  * out_token.  The out arrays may be the in arrays of the same name.
- * 0 <= n_requests, n_requests * beams <= 65536, 1 <= beams <= 32, 1 <= vocab
- * < 2^24, ld >= vocab, eos_id in [0, vocab), alpha finite and >= 0; logits
- * 4-byte, workspace 256-byte aligned. */
+ * 0 <= n_requests, n_requests * beams <= 65535, 1 <= beams <= 32, 1 <= vocab
+ * < 2^24, ld >= vocab, eos_id in [0, vocab), alpha in [0, 32]; logits
+ * 4-byte, workspace 256-byte aligned (NULL when the size call reports 0). */
 typedef struct mtp_beam_args {
     int32_t n_requests, beams, vocab, eos_id, eos_min;
     float alpha;

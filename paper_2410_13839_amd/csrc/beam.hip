@@ -3,8 +3,13 @@
 //   lp[v] = x[v] - (M + log sum_v exp(x[v] - M)),  M = max x
 //
 // A beam's best candidates are its largest logits whatever its normaliser, so
-// one pass per beam row finds both; a second step per request ranks the beams'
-// candidates against each other in float64.
+// one pass over the logits finds both.  One wave takes a chunk of 2048 logits
+// into registers (32 loads in flight a lane), sums their exponentials and
+// keeps the chunk's `beams` best in order: the smallest of (at least `beams`)
+// group maxima bounds the last of them from below, what reaches the bound is
+// gathered into LDS (a few dozen logits) and taken best first.  A request's
+// workgroup then merges the sorted lists of each beam's chunks, and the beams'
+// lists in float64.  With few chunks all of it is one launch.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -15,140 +20,292 @@
 namespace mtp {
 namespace {
 
-constexpr int BT = 256;                  // threads per beam row
 constexpr int MAX_BEAMS = 32;
+constexpr int NV = 32;                   // logits per lane
+constexpr int CHUNK = 64 * NV;           // logits per wave
+constexpr int CAP = 256;                 // gathered candidates per wave
+constexpr int FUSED_UNITS = 32;          // chunks per request up to which one launch does everything
+constexpr float LOG2E = 1.4426950408889634f;
 
 struct BeamWs {
-    double* lse;                         // [rows]
-    float* val;                          // [rows][beams] a row's best logits, best first
-    int32_t* idx;                        // [rows][beams]
+    double* sum;                         // [rows][chunks] sum of exp(x - max)
+    float* max;                          // [rows][chunks]
+    float2* list;                        // [rows][chunks][beams] (logit, index bits), best first
 };
 
+int beam_chunks(int vocab) { return (vocab + CHUNK - 1) / CHUNK; }
+
 uint64_t beam_carve(const mtp_beam_args& a, BeamWs* w) {
-    const uint64_t rows = (uint64_t)a.n_requests * a.beams;
+    const uint64_t units = (uint64_t)a.n_requests * a.beams * beam_chunks(a.vocab);
     uint64_t o = 0;
     auto take = [&](uint64_t bytes) { uint64_t r = o; o = (o + bytes + 255) & ~uint64_t(255); return r; };
-    const uint64_t l = take(rows * 8), v = take(rows * a.beams * 4), i = take(rows * a.beams * 4);
+    if (a.beams * beam_chunks(a.vocab) <= FUSED_UNITS) return 0;
+    const uint64_t s = take(units * 8), m = take(units * 4), l = take(units * a.beams * 8);
     if (w) {
         char* p = (char*)a.workspace;
-        w->lse = (double*)(p + l); w->val = (float*)(p + v); w->idx = (int32_t*)(p + i);
+        w->sum = (double*)(p + s); w->max = (float*)(p + m); w->list = (float2*)(p + l);
     }
     return o;
 }
 
-// The logit as the selection sees it.
-__device__ __forceinline__ float beam_logit(const mtp_beam_args& a, const float* x, int v, bool mask_eos) {
-    const float f = x[v];
-    return (f != f || (mask_eos && v == a.eos_id)) ? -INFINITY : f;
+// Best first: larger value, then lower index.
+__device__ __forceinline__ bool before(float va, int ia, float vb, int ib) {
+    return (va > vb) | ((va == vb) & (ia < ib));
 }
 
-// Best first: larger value, then lower index.
-__device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
+__device__ __forceinline__ float min_f(float a, float b) { return a < b ? a : b; }
 
-__global__ __launch_bounds__(BT) void beam_row_kernel(mtp_beam_args a, BeamWs w) {
-    __shared__ float s_v[BT / 64];
-    __shared__ int s_i[BT / 64];
-    __shared__ double s_s[BT / 64];
-    const int row = blockIdx.x, tid = threadIdx.x;
-    if (a.done[row] > 0) return;
+// One wave: chunk `ch` of row `row`; list[0 .. beams) gets its best logits
+// (-infinity and indexes past the vocabulary behind the chunk's end), mx and
+// sum its normaliser's part.  buf: CAP entries of LDS of this wave.
+__device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int ch, float2* list, float* mx_out,
+                                           double* sum_out, float2* buf) {
+    const int lane = threadIdx.x & 63, W = a.beams;
     const float* x = a.logits + (int64_t)row * a.ld;
-    const bool mask = a.len[row] < a.eos_min;
-    float pv = INFINITY;                 // the last one taken
-    int pi = -1;
-    const int n = min(a.beams, a.vocab);
-    for (int k = 0; k < n; ++k) {
-        float bv = -INFINITY;
-        int bi = 0x7fffffff;
-        for (int v = tid; v < a.vocab; v += BT) {
-            const float f = beam_logit(a, x, v, mask);
-            if (before(pv, pi, f, v) && before(f, v, bv, bi)) { bv = f; bi = v; }
+    const int v0 = ch * CHUNK + lane;
+    const int hide = a.len[row] < a.eos_min ? a.eos_id : -1;
+    float f[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = v0 + 64 * i;
+        f[i] = v < a.vocab ? x[v] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        f[i] = (f[i] != f[i]) | (v0 + 64 * i == hide) ? -INFINITY : f[i];
+        top = fmaxf(top, f[i]);
+    }
+    // maxima of groups of lanes, at least W groups; bound: the smallest of them
+    float grp = top;
+    if (W <= 32) grp = fmaxf(grp, dpp_f<DPP_XOR1>(grp));
+    if (W <= 16) grp = fmaxf(grp, dpp_f<DPP_XOR2>(grp));
+    if (W <= 8) grp = fmaxf(grp, dpp_f<DPP_HALF_MIRROR>(grp));
+    if (W <= 4) grp = fmaxf(grp, dpp_f<DPP_ROR8>(grp));
+    float bound = grp;
+    bound = min_f(bound, dpp_f<DPP_XOR2>(bound));
+    bound = min_f(bound, dpp_f<DPP_HALF_MIRROR>(bound));
+    bound = min_f(bound, dpp_f<DPP_ROR8>(bound));
+    float other, mine = pl_lo16(bound, other);
+    bound = min_f(mine, other);
+    mine = pl_lo32(bound, other);
+    bound = min_f(mine, other);
+    const float m = wave_max64(top);
+    // sums of eight exponentials in float32, their sums in float64 (a chunk without a finite logit adds 0)
+    const float mm = m == -INFINITY ? 0.f : m;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NV; i += 8) {
+        float e = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e += __builtin_amdgcn_exp2f((f[i + j] - mm) * LOG2E);
+        sum += (double)e;
+    }
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) { *mx_out = m; *sum_out = sum; }
+
+    int n = 0;                                   // uniform
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint64_t hit = __ballot(f[i] >= bound);
+        if (hit) {
+            const int at = n + __popcll(hit & ((1ull << lane) - 1));
+            if (f[i] >= bound && at < CAP) buf[at] = make_float2(f[i], __int_as_float(v0 + 64 * i));
+            n += __popcll(hit);
         }
-        wave_argmax(bv, bi);
-        if ((tid & 63) == 0) { s_v[tid >> 6] = bv; s_i[tid >> 6] = bi; }
-        __syncthreads();
-        for (int i = 0; i < BT / 64; ++i)
-            if (i == 0 || before(s_v[i], s_i[i], bv, bi)) { bv = s_v[i]; bi = s_i[i]; }
-        __syncthreads();
-        if (tid == 0) { w.val[(size_t)row * a.beams + k] = bv; w.idx[(size_t)row * a.beams + k] = bi; }
-        pv = bv; pi = bi;
-        if (k == 0) {
-            double s = 0.0;
-            for (int v = tid; v < a.vocab; v += BT) s += (double)expf(beam_logit(a, x, v, mask) - bv);
-            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-            if ((tid & 63) == 0) s_s[tid >> 6] = s;
-            __syncthreads();
-            if (tid == 0) {
-                s = 0.0;
-                for (int i = 0; i < BT / 64; ++i) s += s_s[i];
-                w.lse[row] = (double)bv + log(s);
-            }
+    }
+    __builtin_amdgcn_wave_barrier();
+    float pv = INFINITY;                         // the last one taken
+    int pi = -1;
+    if (n <= CAP) {
+        float cv[CAP / 64];
+        int ci[CAP / 64];
+#pragma unroll
+        for (int k = 0; k < CAP / 64; ++k) {
+            const bool in = 64 * k + lane < n;
+            const float2 e = buf[in ? 64 * k + lane : 0];
+            cv[k] = in ? e.x : -INFINITY;
+            ci[k] = in ? __float_as_int(e.y) : 0x7fffffff;
+        }
+        for (int w = 0; w < W; ++w) {
+            float bv = -INFINITY;
+            int bi = 0x7fffffff;
+#pragma unroll
+            for (int k = 0; k < CAP / 64; ++k)
+                if (before(pv, pi, cv[k], ci[k]) & before(cv[k], ci[k], bv, bi)) { bv = cv[k]; bi = ci[k]; }
+            wave_argmax_uniform(bv, bi);
+            if (lane == 0) list[w] = make_float2(bv, __int_as_float(bi));
+            pv = bv; pi = bi;
+        }
+    } else {
+        // many equal logits: all of the chunk, once per place
+        for (int w = 0; w < W; ++w) {
+            float bv = -INFINITY;
+            int bi = 0x7fffffff;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (before(pv, pi, f[i], v0 + 64 * i) & before(f[i], v0 + 64 * i, bv, bi)) { bv = f[i]; bi = v0 + 64 * i; }
+            wave_argmax_uniform(bv, bi);
+            if (lane == 0) list[w] = make_float2(bv, __int_as_float(bi));
+            pv = bv; pi = bi;
         }
     }
 }
 
-__global__ __launch_bounds__(64) void beam_merge_kernel(mtp_beam_args a, BeamWs w) {
-    __shared__ double s_den[MAX_BEAMS], s_lse[MAX_BEAMS];
-    __shared__ float s_score[MAX_BEAMS];
-    __shared__ int s_len[MAX_BEAMS], s_done[MAX_BEAMS];
-    const int r = blockIdx.x, lane = threadIdx.x, W = a.beams, n = min(W, a.vocab);
-    if (lane < W) {
-        const int row = r * W + lane;
-        const int dn = a.done[row] > 0;
-        const int len = a.len[row] + (dn ? 0 : 1);
-        s_done[lane] = dn; s_len[lane] = len; s_score[lane] = a.score[row];
-        s_lse[lane] = dn ? 0.0 : w.lse[row];
-        s_den[lane] = pow((double)max(len, 1), (double)a.alpha);
+// The waves' own scratch.
+struct BeamLds {
+    double lse[MAX_BEAMS], den[MAX_BEAMS];
+    float score[MAX_BEAMS];
+    int len[MAX_BEAMS], done[MAX_BEAMS];
+    float2 best[MAX_BEAMS][MAX_BEAMS];           // each beam's best logits over its chunks
+};
+
+// A request's merge by a workgroup of NW waves.  max, sum, list: the request's
+// own, [beams][chunks] and [beams][chunks][beams].
+template <int NW>
+__device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const float* max, const double* sum,
+                                           const float2* list, int chunks, BeamLds& s) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.beams, n = min(W, a.vocab);
+    if (threadIdx.x < W) {
+        const int row = r * W + threadIdx.x, dn = a.done[row] > 0, len = a.len[row] + (dn ? 0 : 1);
+        s.done[threadIdx.x] = dn; s.len[threadIdx.x] = len; s.score[threadIdx.x] = a.score[row];
+        s.den[threadIdx.x] = a.alpha == 0.f ? 1.0 : pow((double)::max(len, 1), (double)a.alpha);
     }
     __syncthreads();
-    double pr = INFINITY;
-    int64_t pf = -1;
-    for (int k = 0; k < W; ++k) {
-        double br = -INFINITY, bt = -INFINITY;
-        int64_t bf = INT64_MAX;
-        for (int i = lane; i < W * n; i += 64) {
-            const int b = i / n, j = i % n;
-            int tok;
-            double total;
-            if (s_done[b]) {
-                // itself first, then the tokens it cannot take
-                tok = j == 0 ? a.eos_id : (j - 1 < a.eos_id ? j - 1 : j);
-                total = j == 0 ? (double)s_score[b] : -INFINITY;
-            } else {
-                const size_t at = ((size_t)r * W + b) * W + j;
-                tok = w.idx[at];
-                total = (double)s_score[b] + ((double)w.val[at] - s_lse[b]);
+    for (int b = wave; b < W; b += NW) {
+        if (s.done[b]) continue;                 // uniform over the wave
+        const float* bm = max + (size_t)b * chunks;
+        const double* bs = sum + (size_t)b * chunks;
+        float m = -INFINITY;
+        for (int i = lane; i < chunks; i += 64) m = fmaxf(m, bm[i]);
+        m = wave_max64(m);
+        double t = 0.0;
+        for (int i = lane; i < chunks; i += 64) t += bs[i] * exp((double)bm[i] - (double)m);
+        for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+        if (lane == 0) s.lse[b] = (double)m + log(t);
+        const float2* bl = list + (size_t)b * chunks * W;
+        if (chunks == 1) {
+            if (lane < n) s.best[b][lane] = bl[lane];
+            continue;
+        }
+        // lane i: the heads of the lists of chunks i, i + 64, ... (the best of them, advanced past what was taken)
+        float pv = INFINITY;
+        int pi = -1;
+        float hv = -INFINITY;
+        int hi = 0x7fffffff;
+        bool stale = true;
+        for (int w = 0; w < n; ++w) {
+            if (stale) {
+                hv = -INFINITY; hi = 0x7fffffff;
+                for (int i = lane; i < chunks; i += 64)
+                    for (int k = 0; k < W; ++k) {
+                        const float2 e = bl[(size_t)i * W + k];
+                        const int id = __float_as_int(e.y);
+                        if (before(pv, pi, e.x, id)) {
+                            if (before(e.x, id, hv, hi)) { hv = e.x; hi = id; }
+                            break;
+                        }
+                    }
             }
-            if (!(total < INFINITY)) total = -INFINITY;      // NaN too
-            double rank = total / s_den[b];
-            if (!(rank == rank)) rank = -INFINITY;       // -infinity by an overflowed length term
-            const int64_t flat = (int64_t)b * a.vocab + tok;
-            const bool later = rank < pr || (rank == pr && flat > pf);
-            if (later && (rank > br || (rank == br && flat < bf))) { br = rank; bt = total; bf = flat; }
-        }
-        for (int o = 32; o; o >>= 1) {
-            const double orr = __shfl_xor(br, o), ot = __shfl_xor(bt, o);
-            const int64_t of = __shfl_xor((long long)bf, o);
-            if (orr > br || (orr == br && of < bf)) { br = orr; bt = ot; bf = of; }
-        }
-        pr = br; pf = bf;
-        if (lane == 0) {
-            const int b = (int)(bf / a.vocab), tok = (int)(bf % a.vocab), o = r * W + k;
-            a.out_score[o] = (float)bt;
-            a.out_len[o] = s_len[b];
-            a.out_done[o] = s_done[b] | (tok == a.eos_id ? 1 : 0);
-            a.out_parent[o] = r * W + b;
-            a.out_token[o] = tok;
+            float bv = hv;
+            int bi = hi;
+            wave_argmax_uniform(bv, bi);
+            if (lane == 0) s.best[b][w] = make_float2(bv, __int_as_float(bi));
+            stale = hi == bi;
+            pv = bv; pi = bi;
         }
     }
+    __syncthreads();
+    if (wave != 0) return;
+    // lane b: the head of beam b's list
+    int at = 0, tok = 0;
+    double total = -INFINITY, rank = -INFINITY;
+    int64_t flat = INT64_MAX;
+    const bool own = lane < W;
+    const double lse = own && !s.done[lane] ? s.lse[lane] : 0.0, den = own ? s.den[lane] : 1.0;
+    const float score = own ? s.score[lane] : 0.f;
+    const int dn = own ? s.done[lane] : 0;
+    // a beam without a finite score or normaliser: every candidate is -infinity, in token order
+    const bool dead = own && !dn && !(fabsf(score) < INFINITY && fabs(lse) < INFINITY);
+    auto head = [&]() {
+        flat = INT64_MAX;
+        total = rank = -INFINITY;
+        if (!own || at >= n) return;
+        if (dn) {
+            // itself first, then the tokens that it cannot take
+            tok = at == 0 ? a.eos_id : (at - 1 < a.eos_id ? at - 1 : at);
+            total = at == 0 && score < INFINITY ? (double)score : -INFINITY;     // (NaN: -infinity too)
+        } else if (dead) {
+            tok = at;
+        } else {
+            const float2 e = s.best[lane][at];
+            tok = __float_as_int(e.y);
+            total = (double)score + ((double)e.x - lse);
+        }
+        rank = total / den;
+        flat = (int64_t)lane * a.vocab + tok;
+    };
+    head();
+    for (int k = 0; k < W; ++k) {
+        double br = rank;
+        long long bf = flat;
+        for (int o = 1; o < W; o <<= 1) {
+            const double orr = __shfl_xor(br, o);
+            const long long of = __shfl_xor(bf, o);
+            if (orr > br || (orr == br && of < bf)) { br = orr; bf = of; }
+        }
+        if (own && flat == bf) {                         // one lane: the head that is taken
+            const int o = r * W + k;
+            a.out_score[o] = (float)total;
+            a.out_len[o] = s.len[lane];
+            a.out_done[o] = dn | (tok == a.eos_id ? 1 : 0);
+            a.out_parent[o] = r * W + lane;
+            a.out_token[o] = tok;
+            ++at;
+            head();
+        }
+    }
+}
+
+// One launch per request: few chunks.
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void beam_fused_kernel(mtp_beam_args a) {
+    __shared__ BeamLds s;
+    __shared__ float2 s_buf[NW][CAP], s_list[FUSED_UNITS * MAX_BEAMS];
+    __shared__ float s_max[FUSED_UNITS];
+    __shared__ double s_sum[FUSED_UNITS];
+    const int r = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = a.beams;
+    const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
+    for (int u = wave; u < W * chunks; u += NW) {
+        const int b = u / chunks;
+        if (a.done[r * W + b] > 0) continue;
+        beam_chunk(a, r * W + b, u - b * chunks, s_list + u * W, &s_max[u], &s_sum[u], s_buf[wave]);
+    }
+    __syncthreads();
+    beam_merge<NW>(a, r, s_max, s_sum, s_list, chunks, s);
+}
+
+__global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs w, int chunks) {
+    __shared__ float2 s_buf[4][CAP];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.y, ch = blockIdx.x * 4 + wave;
+    if (ch >= chunks || a.done[row] > 0) return;
+    const size_t u = (size_t)row * chunks + ch;
+    beam_chunk(a, row, ch, w.list + u * a.beams, &w.max[u], &w.sum[u], s_buf[wave]);
+}
+
+__global__ __launch_bounds__(512) void beam_merge_kernel(mtp_beam_args a, BeamWs w, int chunks) {
+    __shared__ BeamLds s;
+    const size_t u = (size_t)blockIdx.x * a.beams * chunks;
+    beam_merge<8>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
 }
 
 bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }
 
 int beam_check(const mtp_beam_args* a) {
     if (!a) return MTP_EINVAL;
-    if (a->beams < 1 || a->beams > MAX_BEAMS || a->n_requests < 0 || (int64_t)a->n_requests * a->beams > 65536 ||
+    if (a->beams < 1 || a->beams > MAX_BEAMS || a->n_requests < 0 || (int64_t)a->n_requests * a->beams > 65535 ||
         a->vocab < 1 || a->vocab >= (1 << 24) || a->eos_id < 0 || a->eos_id >= a->vocab || !(a->alpha >= 0.f) ||
-        !isfinite(a->alpha))
+        a->alpha > 32.f)                         // (2^31)^32 is a finite float64
         return MTP_EINVAL;
     return MTP_OK;
 }
@@ -173,13 +330,21 @@ int mtp_beam_select(const mtp_beam_args* args, void* hip_stream) {
     if (a.n_requests == 0) return MTP_OK;
     if (!aligned(a.logits, 4) || !aligned(a.score, 4) || !aligned(a.len, 4) || !aligned(a.done, 4) ||
         !aligned(a.out_score, 4) || !aligned(a.out_len, 4) || !aligned(a.out_done, 4) || !aligned(a.out_parent, 4) ||
-        !aligned(a.out_token, 4) || !aligned(a.workspace, 256) || a.ld < a.vocab)
+        !aligned(a.out_token, 4) || a.ld < a.vocab)
         return MTP_EINVAL;
     BeamWs w{};
-    if (beam_carve(a, &w) > a.workspace_bytes) return MTP_ENOMEM;
+    const uint64_t need = beam_carve(a, &w);
+    if (need && !aligned(a.workspace, 256)) return MTP_EINVAL;
+    if (need > a.workspace_bytes) return MTP_ENOMEM;
     hipStream_t st = (hipStream_t)hip_stream;
-    hipLaunchKernelGGL(beam_row_kernel, dim3(a.n_requests * a.beams), dim3(BT), 0, st, a, w);
-    hipLaunchKernelGGL(beam_merge_kernel, dim3(a.n_requests), dim3(64), 0, st, a, w);
+    const int chunks = beam_chunks(a.vocab);
+    if (need == 0) {
+        if (a.beams * chunks <= 4) hipLaunchKernelGGL(beam_fused_kernel<4>, dim3(a.n_requests), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(beam_fused_kernel<16>, dim3(a.n_requests), dim3(1024), 0, st, a);
+    } else {
+        hipLaunchKernelGGL(beam_chunk_kernel, dim3((chunks + 3) / 4, a.n_requests * a.beams), dim3(256), 0, st, a, w, chunks);
+        hipLaunchKernelGGL(beam_merge_kernel, dim3(a.n_requests), dim3(512), 0, st, a, w, chunks);
+    }
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
 

@@ -2,10 +2,11 @@
 // cache writes (mtp_pages_write) and page copies (mtp_pages_copy).
 //
 // The plan keeps no free list: a page is free when no row of the new tables
-// keeps it, so the tables themselves are the allocator's state.  Three
-// launches: clear the page bitmap; every row marks the pages that it keeps and
-// stores how many fresh ones it wants; every row takes its fresh pages by rank
-// among the clear bits and writes its table row, slots and positions.
+// keeps it, so the tables themselves are the allocator's state.  Three steps:
+// every row's lengths, fresh pages and running sums (one workgroup); every row
+// marks the pages that it keeps in a bitmap; every row takes its fresh pages by
+// rank among the clear bits and writes its table row, slots and positions.
+// Small plans run the three steps in one workgroup with the bitmap in LDS.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -16,185 +17,277 @@ namespace mtp {
 namespace {
 
 constexpr int PG = 16;                 // tokens per page
-constexpr int PLAN_T = 256;            // threads of the plan's workgroups
 constexpr int MAX_ROWS = 4096;
+constexpr int ROWS_T = 1024;           // threads of the step that takes every row
+constexpr int PLAN_T = 256;            // threads of the other two
+// one launch up to these sizes: table entries, tokens, bitmap words and rows
+constexpr int ONE_ENTRIES = 8192, ONE_WORDS = 8192, ONE_ROWS = 256;
+
+// Row c of the plan: its parent, the parent's cached tokens, its new tokens
+// (the sign bit: its partly filled last page becomes a fresh one), and the
+// fresh pages of the rows before it.
+typedef int4 PlanRow;
+__device__ __forceinline__ int row_new(const PlanRow& r) { return r.z & 0x7fffffff; }
+__device__ __forceinline__ bool row_moved(const PlanRow& r) { return r.z < 0; }
+__device__ __forceinline__ int row_kept(const PlanRow& r) { return r.y / PG + (r.y % PG > 0 && !row_moved(r) ? 1 : 0); }
+__device__ __forceinline__ int row_need(const PlanRow& r) { return (r.y + row_new(r) + PG - 1) / PG; }
 
 struct PlanWs {
     uint32_t* bits;                    // [words] pages kept
-    int32_t* fresh;                    // [n_rows] fresh pages a row wants
-    int32_t* adds;                     // [n_rows] its new tokens (0 for a bad row)
+    PlanRow* rows;                     // [n_rows]
 };
 
 uint64_t plan_words(int num_pages) { return ((uint64_t)num_pages + 31) / 32; }
 
+bool plan_is_one(const mtp_plan_args& a) {
+    return a.n_rows <= ONE_ROWS && plan_words(a.num_pages) <= ONE_WORDS && (int64_t)a.n_rows * a.max_pages <= ONE_ENTRIES &&
+           a.max_tokens <= ONE_ENTRIES;
+}
+
 uint64_t plan_carve(const mtp_plan_args& a, PlanWs* w) {
+    if (plan_is_one(a)) return 0;
     uint64_t o = 0;
     auto take = [&](uint64_t bytes) { uint64_t r = o; o = (o + bytes + 255) & ~uint64_t(255); return r; };
-    const uint64_t b = take(plan_words(a.num_pages) * 4), f = take((uint64_t)a.n_rows * 4), d = take((uint64_t)a.n_rows * 4);
+    const uint64_t b = take(plan_words(a.num_pages) * 4), f = take((uint64_t)a.n_rows * 16);
     if (w) {
         char* p = (char*)a.workspace;
-        w->bits = (uint32_t*)(p + b); w->fresh = (int32_t*)(p + f); w->adds = (int32_t*)(p + d);
+        w->bits = (uint32_t*)(p + b); w->rows = (PlanRow*)(p + f);
     }
     return o;
 }
 
-// What row c continues; L and A are 0 for a bad row (ok false).
-struct PlanRow { int p, L, A; bool ok; };
-__device__ __forceinline__ PlanRow plan_row(const mtp_plan_args& a, int c) {
-    PlanRow r;
-    r.p = a.parent ? a.parent[c] : c;
-    r.A = a.add[c];
-    r.ok = r.p >= 0 && r.p < a.n_rows && r.A >= 0;
-    r.L = r.ok ? a.len[r.p] : 0;
-    r.ok = r.ok && r.L >= 0 && (int64_t)r.L + r.A <= (int64_t)PG * a.max_pages;
-    if (!r.ok) { r.p = 0; r.L = 0; r.A = 0; }
-    return r;
+// Exclusive sums over the workgroup's NT threads; v becomes the sum of the
+// threads before, the result is the total.  buf: NT / 64 values of LDS.
+template <int NT, typename V>
+__device__ __forceinline__ V block_scan(V& v, V* buf) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const V own = v;
+    V x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const V y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();                   // (buf may still be read from the last call)
+    if (lane == 63) buf[wave] = x;
+    __syncthreads();
+    V before = 0, total = 0;
+    for (int i = 0; i < NT / 64; ++i) {
+        before += i < wave ? buf[i] : 0;
+        total += buf[i];
+    }
+    v = before + x - own;
+    return total;
 }
 
-__global__ __launch_bounds__(PLAN_T) void plan_clear_kernel(mtp_plan_args a, PlanWs w) {
-    const uint64_t n = ((uint64_t)a.num_pages + 31) / 32;
-    for (uint64_t i = (uint64_t)blockIdx.x * PLAN_T + threadIdx.x; i < n; i += (uint64_t)gridDim.x * PLAN_T) w.bits[i] = 0u;
-    if (blockIdx.x == 0 && threadIdx.x < 4) a.status[threadIdx.x] = 0;
-}
-
-// Whether an earlier row continues p too (uniform; every thread calls it).
-__device__ __forceinline__ bool plan_follows(const mtp_plan_args& a, int c, int p) {
-    int hit = 0;
-    if (a.parent)
-        for (int i = threadIdx.x; i < c; i += PLAN_T) {
-            const PlanRow r = plan_row(a, i);
-            hit |= (r.ok && r.p == p) ? 1 : 0;
-        }
-    return __syncthreads_or(hit) != 0;
-}
-
-__global__ __launch_bounds__(PLAN_T) void plan_mark_kernel(mtp_plan_args a, PlanWs w) {
-    const int c = blockIdx.x;
-    const PlanRow r = plan_row(a, c);
-    const int full = r.L / PG, part = r.L % PG > 0, need = (r.L + r.A + PG - 1) / PG;
-    const bool follows = part && r.ok && plan_follows(a, c, r.p);
-    const int keep = full + (part && !follows ? 1 : 0);
-    const int32_t* src = a.table_in + (size_t)r.p * a.max_pages;
+// Step 1 by one workgroup of NT threads: rows, row_start, kv_len, status.
+// low: n_rows words of LDS.
+template <int NT, int PER>
+__device__ __forceinline__ void plan_rows(const mtp_plan_args& a, PlanRow* rows, int* low, long long* buf_t, int* buf_f) {
+    const int tid = threadIdx.x, n = a.n_rows;
+    for (int c = tid; c < n; c += NT) low[c] = 0x7fffffff;
+    __syncthreads();
+    PlanRow r[PER];
     int bad = 0;
-    for (int j = threadIdx.x; j < keep; j += PLAN_T) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = tid + NT * k;
+        r[k] = make_int4(0, 0, 0, 0);
+        if (c >= n) continue;
+        int p = a.parent ? a.parent[c] : c;
+        const int A = a.add[c];
+        bool ok = p >= 0 && p < n && A >= 0;
+        if (!ok) p = 0;
+        const int L = a.len[p];
+        ok = ok && L >= 0 && (int64_t)L + A <= (int64_t)PG * a.max_pages;
+        if (ok) {
+            r[k] = make_int4(p, L, A, 0);
+            if (a.parent && L % PG) atomicMin(&low[p], c);
+        }
+        bad += ok ? 0 : 1;
+    }
+    __syncthreads();
+    long long tokens = 0;              // of the slabs before
+    int pages = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        if (NT * k >= n) break;        // uniform
+        const int c = tid + NT * k;
+        const bool in = c < n;
+        if (in && a.parent && r[k].y % PG && low[r[k].x] != c) r[k].z |= (int)0x80000000;
+        long long t = in ? row_new(r[k]) : 0;
+        int f = in ? row_need(r[k]) - row_kept(r[k]) : 0;
+        const long long tt = block_scan<NT>(t, buf_t);
+        const int ff = block_scan<NT>(f, buf_f);
+        if (in) {
+            r[k].w = pages + f;
+            rows[c] = r[k];
+            const long long s = tokens + t;
+            a.row_start[c] = (int)(s < 0x7fffffff ? s : 0x7fffffff);
+            a.kv_len[c] = r[k].y + row_new(r[k]);
+        }
+        tokens += tt;
+        pages += ff;
+    }
+    const int all_bad = block_scan<NT>(bad, buf_f);
+    if (tid == 0) {
+        a.row_start[n] = (int)(tokens < 0x7fffffff ? tokens : 0x7fffffff);
+        a.status[0] = 0;
+        a.status[1] = all_bad;
+        a.status[2] = 0;
+        a.status[3] = 0;
+    }
+}
+
+// Step 2 for row r by `nt` threads (this one is `i`).
+__device__ __forceinline__ void plan_mark(const mtp_plan_args& a, const PlanRow& r, uint32_t* bits, int i, int nt) {
+    const int keep = row_kept(r);
+    const int32_t* src = a.table_in + (size_t)r.x * a.max_pages;
+    int bad = 0;
+    for (int j = i; j < keep; j += nt) {
         const int pg = src[j];
-        if (pg >= 0 && pg < a.num_pages) atomicOr(&w.bits[pg >> 5], 1u << (pg & 31));
+        if (pg >= 0 && pg < a.num_pages) atomicOr(&bits[pg >> 5], 1u << (pg & 31));
         else ++bad;
     }
     if (bad) atomicAdd(&a.status[2], bad);
-    if (threadIdx.x == 0) {
-        w.fresh[c] = need - keep;
-        // (the sign bit tells the next launch that the row's last page moved)
-        w.adds[c] = r.A | (follows ? (int)0x80000000 : 0);
-        a.kv_len[c] = r.L + r.A;
-        if (!r.ok) atomicAdd(&a.status[1], 1);
-    }
 }
 
-__device__ __forceinline__ int64_t wave_sum64_i(int64_t v) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+// The clear bits of word i (pages that nobody keeps).
+__device__ __forceinline__ uint32_t free_bits(const uint32_t* bits, int i, int num_pages) {
+    const uint32_t b = ~bits[i];
+    const int left = num_pages - 32 * i;
+    return left < 32 ? b & ((1u << left) - 1) : b;
 }
 
-__global__ __launch_bounds__(PLAN_T) void plan_assign_kernel(mtp_plan_args a, PlanWs w) {
-    __shared__ int64_t s_f[PLAN_T / 64], s_a[PLAN_T / 64], s_t[PLAN_T / 64];
-    __shared__ int32_t s_free[PLAN_T + 1];       // free pages before each thread's run of words
-    const int c = blockIdx.x, tid = threadIdx.x;
-    // fresh pages and new tokens of the rows before c, and all new tokens
-    int64_t nf = 0, na = 0, nt = 0;
-    for (int i = tid; i < a.n_rows; i += PLAN_T) {
-        const int ad = w.adds[i] & 0x7fffffff;
-        if (i < c) { nf += w.fresh[i]; na += ad; }
-        nt += ad;
-    }
-    nf = wave_sum64_i(nf); na = wave_sum64_i(na); nt = wave_sum64_i(nt);
-    if ((tid & 63) == 0) { s_f[tid >> 6] = nf; s_a[tid >> 6] = na; s_t[tid >> 6] = nt; }
-    // free pages: each thread counts a run of bitmap words
-    const int words = (a.num_pages + 31) / 32, per = (words + PLAN_T - 1) / PLAN_T;
-    const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
-    auto free_bits = [&](int i) {
-        const uint32_t b = ~w.bits[i];
-        return i == words - 1 && (a.num_pages & 31) ? b & ((1u << (a.num_pages & 31)) - 1) : b;
-    };
-    const int want = w.fresh[c];
+// Free pages before each thread's run of `per` words, into before[0 .. NT].
+template <int NT>
+__device__ __forceinline__ void plan_count(const uint32_t* bits, int num_pages, int per, int* before, int* buf) {
+    const int words = (num_pages + 31) / 32, w0 = min((int)threadIdx.x * per, words), w1 = min(w0 + per, words);
     int cnt = 0;
-    if (want > 0)
-        for (int i = w0; i < w1; ++i) cnt += __popc(free_bits(i));
-    s_free[tid + 1] = cnt;
-    if (tid == 0) s_free[0] = 0;
+    for (int i = w0; i < w1; ++i) cnt += __popc(free_bits(bits, i, num_pages));
+    const int all = block_scan<NT>(cnt, buf);
+    before[threadIdx.x] = cnt;
+    if (threadIdx.x == 0) before[NT] = all;
     __syncthreads();
-    for (int o = 1; o < PLAN_T; o <<= 1) {
-        const int v = tid + 1 > o ? s_free[tid + 1 - o] : 0;
-        __syncthreads();
-        s_free[tid + 1] += v;
-        __syncthreads();
-    }
-    nf = na = nt = 0;
-    for (int i = 0; i < PLAN_T / 64; ++i) { nf += s_f[i]; na += s_a[i]; nt += s_t[i]; }
+}
 
-    const PlanRow r = plan_row(a, c);
-    const int total = r.L + r.A, full = r.L / PG, part = r.L % PG > 0, need = (total + PG - 1) / PG;
-    const bool moved = w.adds[c] < 0;
-    const int keep = need - want;
-    const int32_t* src = a.table_in + (size_t)r.p * a.max_pages;
+// The page of rank k among the free ones, -1 past the last.
+template <int NT>
+__device__ __forceinline__ int plan_page(const uint32_t* bits, int num_pages, int per, const int* before, int k) {
+    if (k >= before[NT]) return -1;
+    int lo = 0, hi = NT;               // before[lo] <= k < before[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] <= k) lo = mid; else hi = mid;
+    }
+    k -= before[lo];
+    int i = lo * per;
+    uint32_t b = free_bits(bits, i, num_pages);
+    while (k >= __popc(b)) {
+        k -= __popc(b);
+        b = free_bits(bits, ++i, num_pages);
+    }
+    for (; k > 0; --k) b &= b - 1;
+    return i * 32 + __ffs(b) - 1;
+}
+
+// Step 3's table row by `nt` threads; the caller synchronises before plan_slots.
+template <int NT>
+__device__ __forceinline__ void plan_table(const mtp_plan_args& a, int c, const PlanRow& r, const uint32_t* bits, int per,
+                                           const int* before, int i, int nt) {
+    const int keep = row_kept(r), need = row_need(r);
+    const int32_t* src = a.table_in + (size_t)r.x * a.max_pages;
     int32_t* dst = a.table + (size_t)c * a.max_pages;
     int missing = 0;
-    for (int j = tid; j < a.max_pages; j += PLAN_T) {
+    for (int j = i; j < a.max_pages; j += nt) {
         int pg = -1;
         if (j < keep) {
             pg = src[j];
             if (pg < 0 || pg >= a.num_pages) pg = -1;
         } else if (j < need) {
-            // the page of rank nf + j - keep among the free ones
-            const int64_t k64 = nf + (j - keep);
-            if (k64 >= s_free[PLAN_T]) {
-                ++missing;
-            } else {
-                int k = (int)k64, lo = 0, hi = PLAN_T;      // s_free[lo] <= k < s_free[hi]
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (s_free[mid] <= k) lo = mid; else hi = mid;
-                }
-                k -= s_free[lo];
-                int i = min(lo * per, words);
-                uint32_t b = free_bits(i);
-                while (k >= __popc(b)) { k -= __popc(b); b = free_bits(++i); }
-                for (; k > 0; --k) b &= b - 1;
-                pg = i * 32 + __ffs(b) - 1;
-            }
+            pg = plan_page<NT>(bits, a.num_pages, per, before, r.w + (j - keep));
+            missing += pg < 0 ? 1 : 0;
         }
         dst[j] = pg;
     }
     if (missing) atomicAdd(&a.status[0], missing);
-    __syncthreads();
-    // slots and positions of the row's tokens
+}
+
+// Slots, positions and the page copy of row c, its table row written.
+__device__ __forceinline__ void plan_slots(const mtp_plan_args& a, int c, const PlanRow& r, int64_t t0, int i, int nt) {
+    const int32_t* dst = a.table + (size_t)c * a.max_pages;
     int lost = 0;
-    for (int i = tid; i < r.A; i += PLAN_T) {
-        const int64_t t = na + i;
+    for (int k = i; k < row_new(r); k += nt) {
+        const int64_t t = t0 + k;
         if (t >= a.max_tokens) { ++lost; continue; }
-        const int pos = r.L + i, pg = dst[pos / PG];
+        const int pos = r.y + k, pg = dst[pos / PG];
         a.slots[t] = pg >= 0 ? pg * PG + pos % PG : -1;
         a.positions[t] = pos;
     }
     if (lost) atomicAdd(&a.status[3], lost);
-    // entries behind the last token
-    for (int64_t t = nt + (int64_t)c * PLAN_T + tid; t < a.max_tokens; t += (int64_t)gridDim.x * PLAN_T) {
-        a.slots[t] = -1;
-        a.positions[t] = -1;
-    }
-    if (tid == 0) {
-        a.row_start[c] = (int32_t)(na < 0x7fffffff ? na : 0x7fffffff);
-        if (c == a.n_rows - 1) a.row_start[a.n_rows] = (int32_t)(nt < 0x7fffffff ? nt : 0x7fffffff);
+    if (i == 0) {
         int s = -1, d = -1;
-        if (moved && part) {
-            s = src[full];
-            if (s < 0 || s >= a.num_pages) s = -1;
-            d = dst[full];
-            if (s < 0 || d < 0) s = d = -1;
+        if (row_moved(r)) {
+            s = a.table_in[(size_t)r.x * a.max_pages + r.y / PG];
+            d = dst[r.y / PG];
+            if (s < 0 || s >= a.num_pages || d < 0) s = d = -1;
         }
         a.copies[2 * c] = s;
         a.copies[2 * c + 1] = d;
     }
+}
+
+// -1 behind the last token.
+__device__ __forceinline__ void plan_rest(const mtp_plan_args& a, int64_t tokens, int64_t i, int64_t nt) {
+    for (int64_t t = tokens + i; t < a.max_tokens; t += nt) {
+        a.slots[t] = -1;
+        a.positions[t] = -1;
+    }
+}
+
+__global__ __launch_bounds__(ROWS_T) void plan_rows_kernel(mtp_plan_args a, PlanWs w) {
+    __shared__ int s_low[MAX_ROWS], s_f[ROWS_T / 64];
+    __shared__ long long s_t[ROWS_T / 64];
+    if (blockIdx.x == 0) {
+        plan_rows<ROWS_T, MAX_ROWS / ROWS_T>(a, w.rows, s_low, s_t, s_f);
+        return;
+    }
+    const int words = (a.num_pages + 31) / 32;
+    for (int i = (blockIdx.x - 1) * ROWS_T + threadIdx.x; i < words; i += (gridDim.x - 1) * ROWS_T) w.bits[i] = 0u;
+}
+
+__global__ __launch_bounds__(PLAN_T) void plan_mark_kernel(mtp_plan_args a, PlanWs w) {
+    plan_mark(a, w.rows[blockIdx.x], w.bits, threadIdx.x, PLAN_T);
+}
+
+__global__ __launch_bounds__(PLAN_T) void plan_assign_kernel(mtp_plan_args a, PlanWs w, int per) {
+    __shared__ int s_before[PLAN_T + 1], s_buf[PLAN_T / 64];
+    const int c = blockIdx.x;
+    const PlanRow r = w.rows[c];
+    if (row_need(r) > row_kept(r)) plan_count<PLAN_T>(w.bits, a.num_pages, per, s_before, s_buf);
+    plan_table<PLAN_T>(a, c, r, w.bits, per, s_before, threadIdx.x, PLAN_T);
+    __syncthreads();
+    plan_slots(a, c, r, a.row_start[c], threadIdx.x, PLAN_T);
+    plan_rest(a, a.row_start[a.n_rows], (int64_t)c * PLAN_T + threadIdx.x, (int64_t)gridDim.x * PLAN_T);
+}
+
+// All three steps by one workgroup, a wave per row.
+__global__ __launch_bounds__(ROWS_T) void plan_one_kernel(mtp_plan_args a, int per) {
+    __shared__ uint32_t s_bits[ONE_WORDS];
+    __shared__ PlanRow s_rows[ONE_ROWS];
+    __shared__ int s_low[ONE_ROWS], s_f[ROWS_T / 64], s_before[ROWS_T + 1];
+    __shared__ long long s_t[ROWS_T / 64];
+    const int words = (a.num_pages + 31) / 32, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < words; i += ROWS_T) s_bits[i] = 0u;
+    plan_rows<ROWS_T, 1>(a, s_rows, s_low, s_t, s_f);
+    __syncthreads();
+    for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_mark(a, s_rows[c], s_bits, lane, 64);
+    __syncthreads();
+    plan_count<ROWS_T>(s_bits, a.num_pages, per, s_before, s_f);
+    for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_table<ROWS_T>(a, c, s_rows[c], s_bits, per, s_before, lane, 64);
+    __syncthreads();
+    for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_slots(a, c, s_rows[c], a.row_start[c], lane, 64);
+    plan_rest(a, a.row_start[a.n_rows], threadIdx.x, ROWS_T);
 }
 
 bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }
@@ -208,21 +301,75 @@ int plan_check(const mtp_plan_args* a) {
 }
 
 // ------------------------------------------------------------------ writes
-template <typename T>
-__global__ __launch_bounds__(256) void pages_write_kernel(mtp_write_args a) {
-    const int D = a.cache.head_dim, H = a.cache.n_kv_heads;
-    const int t = blockIdx.x;
-    const int slot = a.slots[t];
-    if (slot < 0 || slot >= a.cache.num_pages * PG) return;
-    T* page = (T*)a.cache.pool + (size_t)(slot / PG) * 2 * H * PG * D;
-    const T* k = (const T*)a.k + (int64_t)t * a.k_stride;
-    const T* v = (const T*)a.v + (int64_t)t * a.v_stride;
-    const int s = slot % PG;
-    for (int i = threadIdx.x; i < H * D; i += 256) {
-        const int h = i / D, d = i % D;
-        page[(size_t)h * PG * D + s * D + d] = k[i];
-        page[(size_t)(H + h) * PG * D + (sizeof(T) == 2 ? d * PG + s : s * D + d)] = v[i];
+//
+// One wave per (group of 16 tokens, KV head).  Keys and fp32 values are rows of
+// the page: 16-byte pieces.  A bf16 page's V block is transposed: the group's
+// values pass through LDS, and where eight tokens in a row go to eight slots in
+// a row that fill a 16-byte piece of every dimension, they are stored as such;
+// other tokens store two bytes a dimension.
+constexpr int WT = 16;                 // tokens per group
+
+template <typename T, int D>
+__global__ __launch_bounds__(64) void pages_write_kernel(mtp_write_args a) {
+    constexpr int PER = 16 / sizeof(T), PCS = D / PER;          // elements of a piece, pieces of a row
+    constexpr int STR = D + 8;                                  // padded LDS row
+    __shared__ __attribute__((aligned(16))) T s_v[sizeof(T) == 2 ? WT * STR : 1];
+    const int H = a.cache.n_kv_heads, h = blockIdx.x % H, t0 = blockIdx.x / H * WT, lane = threadIdx.x;
+    const int n = min(WT, a.n_tokens - t0);
+    const int lim = a.cache.num_pages * PG;
+    int slot = lane < n ? a.slots[t0 + lane] : -1;              // lanes 0 .. 15: the group's slots
+    if (slot < 0 || slot >= lim) slot = -1;
+    T* pool = (T*)a.cache.pool;
+    const size_t blk = (size_t)PG * D;
+#pragma unroll
+    for (int i = 0; i < WT * PCS / 64; ++i) {
+        const int tok = (64 * i + lane) / PCS, pc = (64 * i + lane) % PCS;
+        const int s = __shfl(slot, tok);
+        if (s >= 0) {
+            const int64_t t = t0 + tok;
+            T* page = pool + (size_t)(s / PG) * 2 * H * blk;
+            const uint4 kk = *reinterpret_cast<const uint4*>((const T*)a.k + t * a.k_stride + h * D + pc * PER);
+            const uint4 vv = *reinterpret_cast<const uint4*>((const T*)a.v + t * a.v_stride + h * D + pc * PER);
+            *reinterpret_cast<uint4*>(page + h * blk + (s % PG) * D + pc * PER) = kk;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4*>(&s_v[tok * STR + pc * PER]) = vv;
+            else *reinterpret_cast<uint4*>(page + (H + h) * blk + (s % PG) * D + pc * PER) = vv;
+        }
     }
+    if constexpr (sizeof(T) == 2) {
+        __syncthreads();
+        // half 0, 1: tokens 0 .. 7, 8 .. 15; whole: they fill an aligned run of eight slots of one page
+        const int first = __shfl(slot, lane & 8);
+        const uint64_t run = __ballot(lane < WT && slot >= 0 && slot == first + (lane & 7) && first % 8 == 0);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            if (((run >> (8 * hf)) & 0xff) == 0xff) {
+                const int s = __shfl(slot, 8 * hf);
+                T* vp = pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG;
+#pragma unroll
+                for (int d = lane; d < D; d += 64) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = (uint32_t)s_v[(8 * hf + 2 * j) * STR + d] | (uint32_t)s_v[(8 * hf + 2 * j + 1) * STR + d] << 16;
+                    *reinterpret_cast<uint4*>(vp + d * PG) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else {
+                for (int j = 8 * hf; j < 8 * hf + 8; ++j) {
+                    const int s = __shfl(slot, j);
+                    if (s < 0) continue;
+                    T* vp = pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG;
+#pragma unroll
+                    for (int d = lane; d < D; d += 64) vp[d * PG] = s_v[j * STR + d];
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int D>
+void write_go(hipStream_t st, const mtp_write_args& a) {
+    const unsigned groups = (unsigned)((a.n_tokens + WT - 1) / WT);
+    hipLaunchKernelGGL((pages_write_kernel<T, D>), dim3(groups * a.cache.n_kv_heads), dim3(64), 0, st, a);
 }
 
 // ------------------------------------------------------------------ copies
@@ -271,18 +418,24 @@ int mtp_pages_plan(const mtp_plan_args* args, void* hip_stream) {
     if (a.n_rows == 0) return MTP_OK;
     if ((a.parent && !aligned(a.parent, 4)) || !aligned(a.len, 4) || !aligned(a.add, 4) || !aligned(a.table_in, 4) ||
         !aligned(a.table, 4) || !aligned(a.row_start, 4) || !aligned(a.kv_len, 4) || !aligned(a.copies, 4) ||
-        !aligned(a.status, 4) || !aligned(a.workspace, 256))
+        !aligned(a.status, 4))
         return MTP_EINVAL;
     if (a.max_tokens > 0 && (!aligned(a.slots, 4) || !aligned(a.positions, 4))) return MTP_EINVAL;
     if (a.parent && a.table == a.table_in) return MTP_EINVAL;
     PlanWs w{};
-    if (plan_carve(a, &w) > a.workspace_bytes) return MTP_ENOMEM;
+    const uint64_t need = plan_carve(a, &w);
+    if (need && !aligned(a.workspace, 256)) return MTP_EINVAL;
+    if (need > a.workspace_bytes) return MTP_ENOMEM;
     hipStream_t st = (hipStream_t)hip_stream;
-    const uint64_t words = plan_words(a.num_pages);
-    const unsigned cb = (unsigned)((words + PLAN_T * 4 - 1) / (PLAN_T * 4));
-    hipLaunchKernelGGL(plan_clear_kernel, dim3(cb < 1024 ? cb : 1024), dim3(PLAN_T), 0, st, a, w);
+    const int words = (int)plan_words(a.num_pages);
+    if (need == 0) {
+        hipLaunchKernelGGL(plan_one_kernel, dim3(1), dim3(ROWS_T), 0, st, a, (words + ROWS_T - 1) / ROWS_T);
+        return launched();
+    }
+    const int cb = (words + ROWS_T * 4 - 1) / (ROWS_T * 4);
+    hipLaunchKernelGGL(plan_rows_kernel, dim3(1 + (cb < 256 ? cb : 256)), dim3(ROWS_T), 0, st, a, w);
     hipLaunchKernelGGL(plan_mark_kernel, dim3(a.n_rows), dim3(PLAN_T), 0, st, a, w);
-    hipLaunchKernelGGL(plan_assign_kernel, dim3(a.n_rows), dim3(PLAN_T), 0, st, a, w);
+    hipLaunchKernelGGL(plan_assign_kernel, dim3(a.n_rows), dim3(PLAN_T), 0, st, a, w, (words + PLAN_T - 1) / PLAN_T);
     return launched();
 }
 
@@ -298,10 +451,9 @@ int mtp_pages_write(const mtp_write_args* args, void* hip_stream) {
         a.k_stride % per || a.v_stride % per)
         return MTP_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (a.cache.dtype == MTP_DTYPE_BF16)
-        hipLaunchKernelGGL((pages_write_kernel<uint16_t>), dim3(a.n_tokens), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((pages_write_kernel<float>), dim3(a.n_tokens), dim3(256), 0, st, a);
+    if (((int64_t)a.n_tokens + WT - 1) / WT * a.cache.n_kv_heads >= (1ll << 31)) return MTP_EINVAL;
+    if (a.cache.dtype == MTP_DTYPE_BF16) a.cache.head_dim == 64 ? write_go<bf16_t, 64>(st, a) : write_go<bf16_t, 128>(st, a);
+    else a.cache.head_dim == 64 ? write_go<float, 64>(st, a) : write_go<float, 128>(st, a);
     return launched();
 }
 

@@ -66,13 +66,29 @@ def _ints(t: torch.Tensor, name: str, shape, device) -> int:
     return t.data_ptr()
 
 
+# the current stream's handle without the Stream object around it (3 us of a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _launch(fn, args, device) -> None:
     """fn on torch's current stream of `device` (made the current device for the call)."""
-    if torch.cuda.current_device() == device.index:
-        fn(args, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    if torch.cuda.current_device() == index:
+        fn(args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            fn(args, torch.cuda.current_stream().cuda_stream)
+            fn(args, _raw_stream(index))
+
+
+def _workspace(size, args, device):
+    """Scratch of the size that `size` reports, in args; the caller holds it until the launch."""
+    need = size(args)
+    if not need:
+        return None
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    return ws
 
 
 def _device(t: torch.Tensor, name: str) -> torch.device:
@@ -90,16 +106,17 @@ def _cache(pool: torch.Tensor) -> _b.mtp_cache:
     return _b.mtp_cache(pool.data_ptr(), _DTYPE[pool.dtype], pages, heads, block // PAGE)
 
 
-def _rows(t: torch.Tensor, name: str, pool: torch.Tensor, heads: Optional[int] = None) -> int:
+def _rows(t: torch.Tensor, name: str, pool: torch.Tensor, dim: int, heads: Optional[int] = None) -> int:
     """Token stride of [tokens, heads, head dim] rows in the pool's type."""
-    dim = pool.shape[3] // PAGE
-    if t.dtype != pool.dtype or t.device != pool.device or t.dim() != 3 or t.shape[2] != dim or \
-            (heads is not None and t.shape[1] != heads):
+    shape = t.shape
+    if t.dtype != pool.dtype or t.device != pool.device or len(shape) != 3 or shape[2] != dim or \
+            (heads is not None and shape[1] != heads):
         raise ValueError(f"{name}: {pool.dtype} [tokens, {'heads' if heads is None else heads}, {dim}] on {pool.device}, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.shape[0] and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim)):
+                         f"not {t.dtype} {tuple(shape)} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if shape[0] and (s2 != 1 or (s1 != dim and shape[1] > 1)):
         raise ValueError(f"{name}: a token's heads must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+    return s0 if shape[0] > 1 else shape[1] * dim
 
 
 def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num_pages: int, max_tokens: int,
@@ -126,9 +143,7 @@ def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num
     args = _b.mtp_plan_args(n, m, num_pages, max_tokens, p_par, p_len, p_add, p_in, p_new,
                             base + 4 * 3 * n, base + 4 * 2 * n, tok.data_ptr() or None,
                             tok.data_ptr() + 4 * max_tokens if max_tokens else None, base, base + 4 * (4 * n + 1), None, 0)
-    need = _b.mtp_pages_plan_workspace_size(args)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    ws = _workspace(_b.mtp_pages_plan_workspace_size, args, dev)
     if n == 0:
         small.zero_()
         tok.fill_(-1)
@@ -142,7 +157,8 @@ def write_pages(pool: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: tor
     one layer's pool (mtp_pages_write); slots outside the pool are skipped."""
     dev = _device(pool, "pool")
     cache = _cache(pool)
-    ks, vs = _rows(k, "k", pool, cache.n_kv_heads), _rows(v, "v", pool, cache.n_kv_heads)
+    heads, dim = cache.n_kv_heads, cache.head_dim
+    ks, vs = _rows(k, "k", pool, dim, heads), _rows(v, "v", pool, dim, heads)
     _need(k.shape[0] == v.shape[0], "k and v: the same number of tokens")
     p = _ints(slots, "slots", (k.shape[0],), dev)
     _launch(_b.mtp_pages_write, _b.mtp_write_args(cache, k.shape[0], p, k.data_ptr(), v.data_ptr(), ks, vs), dev)
@@ -172,21 +188,19 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
     what `out` holds (a new `out` starts undefined there)."""
     dev = _device(pool, "pool")
     cache = _cache(pool)
-    qs = _rows(q, "q", pool)
+    dim = cache.head_dim
+    qs = _rows(q, "q", pool, dim)
     _need(table.dim() == 2, "table: [rows, max_pages]")
     n, m = table.shape
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     _need(out.shape == q.shape, "out: q's shape")
-    os = _rows(out, "out", pool)
+    os = _rows(out, "out", pool, dim)
     args = _b.mtp_attention_args(cache, n, m, q.shape[0], q.shape[1], _b.MTP_ATTN_CAUSAL if causal else _b.MTP_ATTN_FULL,
-                                 window, max_kv, cache.head_dim ** -0.5 if scale is None else scale,
+                                 window, max_kv, dim ** -0.5 if scale is None else scale,
                                  _ints(table, "table", (n, m), dev), _ints(row_start, "row_start", (n + 1,), dev),
                                  _ints(kv_len, "kv_len", (n,), dev), q.data_ptr(), out.data_ptr(), qs, os, None, 0)
-    need = _b.mtp_pages_attention_workspace_size(args)
-    if need:
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    ws = _workspace(_b.mtp_pages_attention_workspace_size, args, dev)
     _launch(_b.mtp_pages_attention, args, dev)
     return out
 
@@ -210,9 +224,8 @@ def select_beams(logits: torch.Tensor, score: torch.Tensor, length: torch.Tensor
     args = _b.mtp_beam_args(r, w, v, eos_id, eos_min, alpha, logits.data_ptr(), ld, score.data_ptr(),
                             _ints(length, "length", (r, w), dev), _ints(done, "done", (r, w), dev), base, base + step,
                             base + 2 * step, base + 3 * step, base + 4 * step, None, 0)
-    need = _b.mtp_beam_select_workspace_size(args)
-    if need:
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        args.workspace, args.workspace_bytes = ws.data_ptr(), need
+    ws = _workspace(_b.mtp_beam_select_workspace_size, args, dev)
     _launch(_b.mtp_beam_select, args, dev)
-    return BeamStep(new[0].view(torch.float32), new[1], new[2], new[3], new[4])
+    del ws
+    new = new.unbind(0)
+    return BeamStep(new[0].view(torch.float32), *new[1:])

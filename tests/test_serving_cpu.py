@@ -25,7 +25,7 @@ BAD_CACHE = [dict(pool=0), dict(pool=4104), dict(dtype=2), dict(dtype=-1), dict(
 
 def _plan(**kw):
     from paper_2410_13839_amd import binding as b
-    a = b.mtp_plan_args(2, 4, 64, 8, None, 256, 512, 768, 1024, 2048, 2304, 2560, 2816, 3136, 3328, 4096, 1 << 20)
+    a = b.mtp_plan_args(2, 5000, 64, 8, None, 256, 512, 768, 1024, 2048, 2304, 2560, 2816, 3136, 3328, 4096, 1 << 20)
     for k, v in kw.items():
         setattr(a, k, v)
     return a
@@ -42,7 +42,7 @@ def _attention(cache=None, **kw):
 
 def _beam(**kw):
     from paper_2410_13839_amd import binding as b
-    a = b.mtp_beam_args(2, 4, 1025, 1024, 0, 0.0, 256, 1025, 512, 768, 1024, 1280, 1536, 1792, 2048, 2304, 4096, 1 << 20)
+    a = b.mtp_beam_args(2, 4, 40000, 39999, 0, 0.0, 256, 40000, 512, 768, 1024, 1280, 1536, 1792, 2048, 2304, 4096, 1 << 20)
     for k, v in kw.items():
         setattr(a, k, v)
     return a
@@ -142,8 +142,8 @@ def test_attention_workspace():
 
 
 @pytest.mark.parametrize("kw", [dict(beams=0), dict(beams=33), dict(n_requests=-1), dict(n_requests=20000), dict(vocab=0),
-                                dict(vocab=1 << 24), dict(eos_id=-1), dict(eos_id=1025), dict(alpha=-0.1), dict(alpha=INF),
-                                dict(alpha=NAN), dict(ld=1024), dict(logits=0), dict(logits=258), dict(score=0),
+                                dict(vocab=1 << 24), dict(eos_id=-1), dict(eos_id=40000), dict(alpha=-0.1), dict(alpha=32.5), dict(alpha=INF),
+                                dict(alpha=NAN), dict(ld=39999), dict(logits=0), dict(logits=258), dict(score=0),
                                 dict(len=0), dict(done=0), dict(out_score=0), dict(out_len=0), dict(out_done=0),
                                 dict(out_parent=0), dict(out_token=0), dict(workspace=0), dict(workspace=4097)])
 def test_beam_select_refuses(kw):
