@@ -152,6 +152,33 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
     }
 }
 
+// One wave: the n best of `entries` <= 64 N (logit, index bits) pairs.
+template <int N>
+__device__ __forceinline__ void best_of_list(const float2* list, int entries, int n, float2* out) {
+    const int lane = threadIdx.x & 63;
+    float f[N];
+    int id[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool in = 64 * i + lane < entries;
+        const float2 e = list[in ? 64 * i + lane : 0];
+        f[i] = in ? e.x : -INFINITY;
+        id[i] = in ? __float_as_int(e.y) : 0x7fffffff;
+    }
+    float pv = INFINITY;
+    int pi = -1;
+    for (int w = 0; w < n; ++w) {
+        float bv = -INFINITY;
+        int bi = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (before(pv, pi, f[i], id[i]) & before(f[i], id[i], bv, bi)) { bv = f[i]; bi = id[i]; }
+        wave_argmax_uniform(bv, bi);
+        if (lane == 0) out[w] = make_float2(bv, __int_as_float(bi));
+        pv = bv; pi = bi;
+    }
+}
+
 // The waves' own scratch.
 struct BeamLds {
     double lse[MAX_BEAMS], den[MAX_BEAMS];
@@ -160,18 +187,21 @@ struct BeamLds {
     float2 best[MAX_BEAMS][MAX_BEAMS];           // each beam's best logits over its chunks
 };
 
+// The request's state (the caller synchronises).
+__device__ __forceinline__ void beam_state(const mtp_beam_args& a, int r, BeamLds& s) {
+    if ((int)threadIdx.x >= a.beams) return;
+    const int row = r * a.beams + threadIdx.x, dn = a.done[row] > 0, len = a.len[row] + (dn ? 0 : 1);
+    s.done[threadIdx.x] = dn; s.len[threadIdx.x] = len; s.score[threadIdx.x] = a.score[row];
+    s.den[threadIdx.x] = a.alpha == 0.f ? 1.0 : pow((double)max(len, 1), (double)a.alpha);
+}
+
 // A request's merge by a workgroup of NW waves.  max, sum, list: the request's
-// own, [beams][chunks] and [beams][chunks][beams].
-template <int NW>
+// own, [beams][chunks] and [beams][chunks][beams].  FEW: at most 256 list
+// entries a beam.
+template <int NW, bool FEW>
 __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const float* max, const double* sum,
                                            const float2* list, int chunks, BeamLds& s) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.beams, n = min(W, a.vocab);
-    if (threadIdx.x < W) {
-        const int row = r * W + threadIdx.x, dn = a.done[row] > 0, len = a.len[row] + (dn ? 0 : 1);
-        s.done[threadIdx.x] = dn; s.len[threadIdx.x] = len; s.score[threadIdx.x] = a.score[row];
-        s.den[threadIdx.x] = a.alpha == 0.f ? 1.0 : pow((double)::max(len, 1), (double)a.alpha);
-    }
-    __syncthreads();
     for (int b = wave; b < W; b += NW) {
         if (s.done[b]) continue;                 // uniform over the wave
         const float* bm = max + (size_t)b * chunks;
@@ -186,6 +216,15 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
         const float2* bl = list + (size_t)b * chunks * W;
         if (chunks == 1) {
             if (lane < n) s.best[b][lane] = bl[lane];
+            continue;
+        }
+        const int entries = chunks * W;
+        if (FEW || entries <= 64 * 4) {
+            best_of_list<4>(bl, entries, n, s.best[b]);
+            continue;
+        }
+        if (entries <= 64 * NV) {
+            best_of_list<NV>(bl, entries, n, s.best[b]);
             continue;
         }
         // lane i: the heads of the lists of chunks i, i + 64, ... (the best of them, advanced past what was taken)
@@ -276,13 +315,14 @@ __global__ __launch_bounds__(64 * NW) void beam_fused_kernel(mtp_beam_args a) {
     __shared__ double s_sum[FUSED_UNITS];
     const int r = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = a.beams;
     const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
+    beam_state(a, r, s);
     for (int u = wave; u < W * chunks; u += NW) {
         const int b = u / chunks;
         if (a.done[r * W + b] > 0) continue;
         beam_chunk(a, r * W + b, u - b * chunks, s_list + u * W, &s_max[u], &s_sum[u], s_buf[wave]);
     }
     __syncthreads();
-    beam_merge<NW>(a, r, s_max, s_sum, s_list, chunks, s);
+    beam_merge<NW, true>(a, r, s_max, s_sum, s_list, chunks, s);
 }
 
 __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs w, int chunks) {
@@ -296,7 +336,9 @@ __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs
 __global__ __launch_bounds__(512) void beam_merge_kernel(mtp_beam_args a, BeamWs w, int chunks) {
     __shared__ BeamLds s;
     const size_t u = (size_t)blockIdx.x * a.beams * chunks;
-    beam_merge<8>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
+    beam_state(a, blockIdx.x, s);
+    __syncthreads();
+    beam_merge<8, false>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
 }
 
 bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }

@@ -172,7 +172,7 @@ __device__ __forceinline__ int dim_of(int dt, int g, int e) {
 }
 
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_args a, AttnGeo g) {
+__global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : 2) void attn_rows_kernel(mtp_attention_args a, AttnGeo g) {
     constexpr int QR = 16, ND = D / 16;
     extern __shared__ __attribute__((aligned(16))) float s_acc[];    // [NW][16][D], dimensions in order
     __shared__ float s_m[NW][QR], s_l[NW][QR];
@@ -717,7 +717,8 @@ int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
 
 // The cut of a call: kernel, tile shape, runs and the workspace of the partial
 // sums.
-struct AttnCut { AttnGeo g; bool wide; uint64_t acc_bytes, bytes; };
+constexpr int ONE_KEYS = 2048;
+struct AttnCut { AttnGeo g; bool wide, one; uint64_t acc_bytes, bytes; };
 
 AttnCut attn_cut(const mtp_attention_args& a) {
     AttnCut x{};
@@ -730,7 +731,9 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     x.g.tt = rt / x.g.gs;
     x.g.n_tiles = a.n_tokens / x.g.tt + a.n_rows;
     const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
-    int64_t n = std::min<int64_t>((512 + work - 1) / work, kv / key_min);
+    // few tiles over few keys: 16 waves a tile and one launch
+    x.one = !x.wide && work <= 256 && kv <= ONE_KEYS;
+    int64_t n = x.one ? 1 : std::min<int64_t>((512 + work - 1) / work, kv / key_min);
     n = std::max<int64_t>(1, std::min<int64_t>(n, 256));
     x.g.n_splits = (int)n;
     x.g.split_len = (int)(((kv + n - 1) / n + KB - 1) / KB * KB);
@@ -789,6 +792,10 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream) {
     hipStream_t st = (hipStream_t)hip_stream;
     const bool bf = a.cache.dtype == MTP_DTYPE_BF16;
     if (x.wide) return a.cache.head_dim == 64 ? tile_go<64>(st, a, x.g) : tile_go<128>(st, a, x.g);
+    if (x.one) {
+        if (a.cache.head_dim == 64) return bf ? rows_go<bf16_t, 64, 16>(st, a, x.g) : rows_go<float, 64, 8>(st, a, x.g);
+        return bf ? rows_go<bf16_t, 128, 8>(st, a, x.g) : rows_go<float, 128, 8>(st, a, x.g);
+    }
     if (a.cache.head_dim == 64) return bf ? rows_go<bf16_t, 64, 4>(st, a, x.g) : rows_go<float, 64, 4>(st, a, x.g);
     return bf ? rows_go<bf16_t, 128, 4>(st, a, x.g) : rows_go<float, 128, 4>(st, a, x.g);
 }

@@ -302,74 +302,87 @@ int plan_check(const mtp_plan_args* a) {
 
 // ------------------------------------------------------------------ writes
 //
-// One wave per (group of 16 tokens, KV head).  Keys and fp32 values are rows of
-// the page: 16-byte pieces.  A bf16 page's V block is transposed: the group's
-// values pass through LDS, and where eight tokens in a row go to eight slots in
-// a row that fill a 16-byte piece of every dimension, they are stored as such;
-// other tokens store two bytes a dimension.
-constexpr int WT = 16;                 // tokens per group
+// One workgroup per (group of tokens, KV head).  Keys and fp32 values are rows
+// of the page: 16-byte pieces.  A bf16 page's V block is transposed: the
+// group's values pass through LDS, and eight tokens in a row that go to eight
+// slots in a row from a multiple of eight on (an octet) are stored as one
+// 16-byte piece per dimension; other tokens store two bytes a dimension.  An
+// octet belongs to its first token's group, which also loads the up to seven
+// tokens behind its own; every group looks at 7 + 48 + 7 slots, a lane each, so
+// that all agree on the octets wherever the groups' borders fall.
+constexpr int WOWN = 48, WEXT = 7;     // a group's own tokens, tokens looked at on either side
 
 template <typename T, int D>
-__global__ __launch_bounds__(64) void pages_write_kernel(mtp_write_args a) {
+__global__ __launch_bounds__(256) void pages_write_kernel(mtp_write_args a) {
     constexpr int PER = 16 / sizeof(T), PCS = D / PER;          // elements of a piece, pieces of a row
     constexpr int STR = D + 8;                                  // padded LDS row
-    __shared__ __attribute__((aligned(16))) T s_v[sizeof(T) == 2 ? WT * STR : 1];
-    const int H = a.cache.n_kv_heads, h = blockIdx.x % H, t0 = blockIdx.x / H * WT, lane = threadIdx.x;
-    const int n = min(WT, a.n_tokens - t0);
+    constexpr bool TURN = sizeof(T) == 2;
+    __shared__ __attribute__((aligned(16))) T s_v[TURN ? (WOWN + WEXT) * STR : 1];
+    __shared__ int s_slot[64];
+    const int H = a.cache.n_kv_heads, h = blockIdx.x % H, t0 = blockIdx.x / H * WOWN, tid = threadIdx.x, lane = tid & 63;
     const int lim = a.cache.num_pages * PG;
-    int slot = lane < n ? a.slots[t0 + lane] : -1;              // lanes 0 .. 15: the group's slots
+    // lane i: token t0 - 7 + i (every wave looks for itself)
+    const int64_t tl = (int64_t)t0 - WEXT + lane;
+    int slot = lane < WOWN + 2 * WEXT && tl >= 0 && tl < a.n_tokens ? a.slots[tl] : -1;
     if (slot < 0 || slot >= lim) slot = -1;
+    if (tid < 64) s_slot[tid] = slot;
+    uint64_t heads = 0, covered = 0;                            // bit i: lane i's token
+    if constexpr (TURN) {
+        const int next = __shfl_down(slot, 1);
+        const uint64_t follows = __ballot(lane < 63 && slot >= 0 && next == slot + 1);
+        heads = __ballot(slot >= 0 && slot % 8 == 0 && lane <= 63 - 8 && ((follows >> lane) & 0x7f) == 0x7f);
+        covered = heads | heads << 1;
+        covered |= covered << 2;
+        covered |= covered << 4;
+        heads &= ((1ull << WOWN) - 1) << WEXT;
+    }
+    __syncthreads();
     T* pool = (T*)a.cache.pool;
     const size_t blk = (size_t)PG * D;
-#pragma unroll
-    for (int i = 0; i < WT * PCS / 64; ++i) {
-        const int tok = (64 * i + lane) / PCS, pc = (64 * i + lane) % PCS;
-        const int s = __shfl(slot, tok);
-        if (s >= 0) {
-            const int64_t t = t0 + tok;
-            T* page = pool + (size_t)(s / PG) * 2 * H * blk;
-            const uint4 kk = *reinterpret_cast<const uint4*>((const T*)a.k + t * a.k_stride + h * D + pc * PER);
-            const uint4 vv = *reinterpret_cast<const uint4*>((const T*)a.v + t * a.v_stride + h * D + pc * PER);
-            *reinterpret_cast<uint4*>(page + h * blk + (s % PG) * D + pc * PER) = kk;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4*>(&s_v[tok * STR + pc * PER]) = vv;
-            else *reinterpret_cast<uint4*>(page + (H + h) * blk + (s % PG) * D + pc * PER) = vv;
-        }
+    for (int i = tid; i < (TURN ? WOWN + WEXT : WOWN) * PCS; i += 256) {
+        const int tok = i / PCS, pc = i % PCS, s = s_slot[WEXT + tok];
+        if (s < 0) continue;
+        const int64_t t = t0 + tok;
+        T* page = pool + (size_t)(s / PG) * 2 * H * blk;
+        if (tok < WOWN)
+            *reinterpret_cast<uint4*>(page + h * blk + (s % PG) * D + pc * PER) =
+                *reinterpret_cast<const uint4*>((const T*)a.k + t * a.k_stride + h * D + pc * PER);
+        const uint4 vv = *reinterpret_cast<const uint4*>((const T*)a.v + t * a.v_stride + h * D + pc * PER);
+        if constexpr (TURN) *reinterpret_cast<uint4*>(&s_v[tok * STR + pc * PER]) = vv;
+        else *reinterpret_cast<uint4*>(page + (H + h) * blk + (s % PG) * D + pc * PER) = vv;
     }
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (TURN) {
         __syncthreads();
-        // half 0, 1: tokens 0 .. 7, 8 .. 15; whole: they fill an aligned run of eight slots of one page
-        const int first = __shfl(slot, lane & 8);
-        const uint64_t run = __ballot(lane < WT && slot >= 0 && slot == first + (lane & 7) && first % 8 == 0);
+        // octets two at a time: those of one page make 32 bytes in a row per dimension
+        while (heads) {
+            const int i0 = __ffsll((unsigned long long)heads) - 1;
+            heads &= heads - 1;
+            const int i1 = heads ? __ffsll((unsigned long long)heads) - 1 : -1;
+            heads &= heads - 1;                                 // (0 stays 0)
+            const int at = tid & 1 ? i1 : i0;
+            if (at < 0) continue;
+            const int s = s_slot[at];
+            T* vp = pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG;
+            const T* row = &s_v[(at - WEXT) * STR];
+            for (int d = tid >> 1; d < D; d += 128) {
+                uint32_t w[4];
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            if (((run >> (8 * hf)) & 0xff) == 0xff) {
-                const int s = __shfl(slot, 8 * hf);
-                T* vp = pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG;
-#pragma unroll
-                for (int d = lane; d < D; d += 64) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        w[j] = (uint32_t)s_v[(8 * hf + 2 * j) * STR + d] | (uint32_t)s_v[(8 * hf + 2 * j + 1) * STR + d] << 16;
-                    *reinterpret_cast<uint4*>(vp + d * PG) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            } else {
-                for (int j = 8 * hf; j < 8 * hf + 8; ++j) {
-                    const int s = __shfl(slot, j);
-                    if (s < 0) continue;
-                    T* vp = pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG;
-#pragma unroll
-                    for (int d = lane; d < D; d += 64) vp[d * PG] = s_v[j * STR + d];
-                }
+                for (int j = 0; j < 4; ++j) w[j] = (uint32_t)row[2 * j * STR + d] | (uint32_t)row[(2 * j + 1) * STR + d] << 16;
+                *reinterpret_cast<uint4*>(vp + d * PG) = make_uint4(w[0], w[1], w[2], w[3]);
             }
+        }
+        for (int i = tid; i < WOWN * D; i += 256) {
+            const int tok = i / D, d = i % D, s = s_slot[WEXT + tok];
+            if (s < 0 || (covered >> (WEXT + tok) & 1)) continue;
+            pool[(size_t)(s / PG) * 2 * H * blk + (H + h) * blk + d * PG + s % PG] = s_v[tok * STR + d];
         }
     }
 }
 
 template <typename T, int D>
 void write_go(hipStream_t st, const mtp_write_args& a) {
-    const unsigned groups = (unsigned)((a.n_tokens + WT - 1) / WT);
-    hipLaunchKernelGGL((pages_write_kernel<T, D>), dim3(groups * a.cache.n_kv_heads), dim3(64), 0, st, a);
+    const unsigned groups = (unsigned)((a.n_tokens + WOWN - 1) / WOWN);
+    hipLaunchKernelGGL((pages_write_kernel<T, D>), dim3(groups * a.cache.n_kv_heads), dim3(256), 0, st, a);
 }
 
 // ------------------------------------------------------------------ copies
@@ -451,7 +464,7 @@ int mtp_pages_write(const mtp_write_args* args, void* hip_stream) {
         a.k_stride % per || a.v_stride % per)
         return MTP_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (((int64_t)a.n_tokens + WT - 1) / WT * a.cache.n_kv_heads >= (1ll << 31)) return MTP_EINVAL;
+    if (((int64_t)a.n_tokens + WOWN - 1) / WOWN * a.cache.n_kv_heads >= (1ll << 31)) return MTP_EINVAL;
     if (a.cache.dtype == MTP_DTYPE_BF16) a.cache.head_dim == 64 ? write_go<bf16_t, 64>(st, a) : write_go<bf16_t, 128>(st, a);
     else a.cache.head_dim == 64 ? write_go<float, 64>(st, a) : write_go<float, 128>(st, a);
     return launched();

@@ -369,7 +369,8 @@ def check_beams(logits, score, length, done, eos, eos_min=0, alpha=0.0):
 
 
 @pytest.mark.parametrize("R,W,V", [(1, 1, 1), (1, 1, 2), (2, 4, 3), (1, 4, 1025), (3, 8, 1000), (5, 32, 777), (2, 5, 33000),
-                                   (40, 2, 64), (1, 16, 131072), (1, 32, 20), (9, 3, 4097)])
+                                   (40, 2, 64), (1, 16, 131072), (1, 32, 20), (9, 3, 4097), (2, 32, 9000), (1, 8, 1 << 20),
+                                   (2, 9, 60001)])
 @pytest.mark.parametrize("alpha,eos_min", [(0.0, 0), (0.7, 12)])
 def test_beam_select(R, W, V, alpha, eos_min):
     rng = np.random.default_rng(R * W + V)
