@@ -23,6 +23,7 @@ namespace {
 
 constexpr int PG = 16;
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int MAX_RUNS = 256;                    // of a tile's keys
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
@@ -127,6 +128,8 @@ __device__ __forceinline__ uint32_t finite2(uint32_t v, uint32_t& seen) {
 // transposed V block.  fp32 (16 keys a product): the contraction's index g of
 // step e is dimension 16 j + 4 g + e, or key 4 g + e, and row r of the output
 // tile dt is dimension (D / 16) r + dt, all 16-byte loads again.
+constexpr int NW = 4;
+
 template <typename T, int D>
 struct Keys;                                     // 32 keys in operand order
 
@@ -171,10 +174,10 @@ __device__ __forceinline__ int dim_of(int dt, int g, int e) {
     return sizeof(T) == 2 ? 16 * dt + 4 * g + e : (D / 16) * (4 * g + e) + dt;
 }
 
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : 2) void attn_rows_kernel(mtp_attention_args a, AttnGeo g) {
+template <typename T, int D>
+__global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_args a, AttnGeo g) {
     constexpr int QR = 16, ND = D / 16;
-    extern __shared__ __attribute__((aligned(16))) float s_acc[];    // [NW][16][D], dimensions in order
+    __shared__ __attribute__((aligned(16))) float s_acc[NW * QR * D];     // [wave][row][dimensions in order]
     __shared__ float s_m[NW][QR], s_l[NW][QR];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, gr = lane >> 4;
@@ -656,54 +659,71 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
     }
 }
 
-// Joins a tile's runs: one workgroup per (tile, head block), RT rows a tile.
+// Joins a tile's runs: one wave per query row.  The runs' weights exp2(m_s - m)
+// once (lane i: runs i, i + 64, ...), then every group of D / 4 lanes takes
+// runs in turn, its loads independent of each other.
+constexpr int JW = 4;                            // waves (rows) of a workgroup
+
 template <typename T, int D, int RT>
-__global__ __launch_bounds__(256) void attn_join_kernel(mtp_attention_args a, AttnGeo g) {
-    const int H = a.cache.n_kv_heads, HB = H * g.hb;
-    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb;
+__global__ __launch_bounds__(64 * JW) void attn_join_kernel(mtp_attention_args a, AttnGeo g) {
+    constexpr int LD = D / 4, SG = 64 / LD;      // lanes of a row's dimensions, runs at a time
+    __shared__ float s_w[JW][MAX_RUNS];
+    const int H = a.cache.n_kv_heads, HB = H * g.hb, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb, qr = blockIdx.y * JW + wave;
     const AttnTile t = find_tile(a, g, tile);
-    if (t.nt == 0) return;
+    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs, heads = min(g.gs, group - h0);
+    if (qr >= t.nt * g.gs || qr % g.gs >= heads) return;
     int k0, k1;
     const int live = runs_of(g, t, 0, k0, k1);
     if (live <= 1) return;
-    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs, heads = min(g.gs, group - h0), rows = t.nt * g.gs;
-    const size_t slot = (size_t)blockIdx.x * g.n_splits * RT;
-    for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
-        const int qr = i / (D / 4), d = (i - qr * (D / 4)) * 4;
-        if (qr % g.gs >= heads) continue;
-        float m = -INFINITY, l = 0.f;
-        f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < live; ++s) {
-            const float2 x = g.ml[slot + (size_t)s * RT + qr];
-            if (x.x == -INFINITY && x.y == 0.f) continue;
-            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(&g.acc[(slot + (size_t)s * RT + qr) * D + d]);
-            const float mn = fmaxf(m, x.x);
-            const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-            const float f1 = x.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x.x - mn);
-            l = l * f0 + x.y * f1;
-            v = (m == -INFINITY ? f32x4_t{0.f, 0.f, 0.f, 0.f} : v * f0) + w * f1;
-            m = mn;
-        }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* op = (T*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + d;
-        if constexpr (sizeof(T) == 2)
-            *reinterpret_cast<uint2*>(op) = make_uint2(pk2(v[0] * inv, v[1] * inv), pk2(v[2] * inv, v[3] * inv));
-        else
-            *reinterpret_cast<f32x4_t*>(op) = v * inv;
+    const size_t slot = (size_t)blockIdx.x * g.n_splits * RT + qr;
+    // (a run that the row sees nothing of has m = -infinity and l = 0; one whose scores are not numbers l = NaN)
+    float2 x[MAX_RUNS / 64];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAX_RUNS / 64; ++i) {
+        x[i] = make_float2(-INFINITY, 0.f);
+        if (64 * i + lane < live) x[i] = g.ml[slot + (size_t)(64 * i + lane) * RT];
+        m = fmaxf(m, x[i].x);
     }
+    m = wave_max64(m);
+#pragma unroll
+    for (int i = 0; i < MAX_RUNS / 64; ++i) {
+        const float w = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[i].x - m);
+        l += x[i].x == -INFINITY ? x[i].y : w * x[i].y;
+        s_w[wave][64 * i + lane] = w;
+    }
+    l = wave_sum64(l);
+    __builtin_amdgcn_wave_barrier();
+    const int sg = lane / LD, d = (lane - sg * LD) * 4;
+    f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = sg; s < live; s += SG) {
+        const float w = s_w[wave][s];
+        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(&g.acc[(slot + (size_t)s * RT) * D + d]);
+        if (w != 0.f) v += o * w;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (LD == 16) v[e] = xor16_sum(v[e]);
+        v[e] = xor32_sum(v[e]);
+    }
+    if (sg != 0) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* op = (T*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + d;
+    if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(op) = make_uint2(pk2(v[0] * inv, v[1] * inv), pk2(v[2] * inv, v[3] * inv));
+    else
+        *reinterpret_cast<f32x4_t*>(op) = v * inv;
 }
 
 // ------------------------------------------------------------------- launches
-template <typename T, int D, int NW>
+template <typename T, int D>
 int rows_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
-    const size_t lds = (size_t)NW * 16 * D * 4;
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
-    if (lds > 64 * 1024 &&
-        hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_rows_kernel<T, D, NW>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
-        return MTP_EHIP;
-    hipLaunchKernelGGL((attn_rows_kernel<T, D, NW>), dim3(work, g.n_splits), dim3(64 * NW), lds, st, a, g);
-    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<T, D, 16>), dim3(work), dim3(256), 0, st, a, g);
+    hipLaunchKernelGGL((attn_rows_kernel<T, D>), dim3(work, g.n_splits), dim3(64 * NW), 0, st, a, g);
+    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<T, D, 16>), dim3(work, (g.tt * g.gs + JW - 1) / JW), dim3(64 * JW), 0, st, a, g);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
 
@@ -711,14 +731,13 @@ template <int D>
 int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
     hipLaunchKernelGGL((attn_tile_kernel<D>), dim3((work * g.n_splits + 7) / 8 * 8), dim3(256), 0, st, a, g);
-    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<bf16_t, D, TR>), dim3(work), dim3(256), 0, st, a, g);
+    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<bf16_t, D, TR>), dim3(work, (g.tt * g.gs + JW - 1) / JW), dim3(64 * JW), 0, st, a, g);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
 
 // The cut of a call: kernel, tile shape, runs and the workspace of the partial
 // sums.
-constexpr int ONE_KEYS = 2048;
-struct AttnCut { AttnGeo g; bool wide, one; uint64_t acc_bytes, bytes; };
+struct AttnCut { AttnGeo g; bool wide; uint64_t acc_bytes, bytes; };
 
 AttnCut attn_cut(const mtp_attention_args& a) {
     AttnCut x{};
@@ -726,15 +745,29 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     x.g.hb = (group + 15) / 16;
     x.g.gs = (group + x.g.hb - 1) / x.g.hb;
     const int64_t kv_all = (int64_t)PG * a.max_pages, kv = a.max_kv > 0 && a.max_kv < kv_all ? a.max_kv : kv_all;
-    x.wide = a.cache.dtype == MTP_DTYPE_BF16 && (int64_t)a.n_tokens * x.g.gs > 32ll * a.n_rows;
-    const int rt = x.wide ? TR : 16, key_min = x.wide ? 512 : 256;
+    // The wide kernel from this many query rows a cache row on (16 rows, 8 KV heads, 1000 to 4000 keys: head dim 128, 8
+    // rows 54.5 us wide and 57.8 us narrow, 4 rows of 32 sequences 309 and 224 us; head dim 64, 64 rows 55 and 57 us,
+    // 48 rows 57 and 46 us).
+    const bool d128 = a.cache.head_dim == 128;
+    x.wide = a.cache.dtype == MTP_DTYPE_BF16 && (int64_t)a.n_tokens * x.g.gs >= (d128 ? 8ll : 64ll) * a.n_rows;
+    const int rt = x.wide ? TR : 16;
     x.g.tt = rt / x.g.gs;
     x.g.n_tiles = a.n_tokens / x.g.tt + a.n_rows;
     const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
-    // few tiles over few keys: 16 waves a tile and one launch
-    x.one = !x.wide && work <= 256 && kv <= ONE_KEYS;
-    int64_t n = x.one ? 1 : std::min<int64_t>((512 + work - 1) / work, kv / key_min);
-    n = std::max<int64_t>(1, std::min<int64_t>(n, 256));
+    // Runs of the keys: as many workgroups as the CUs hold at once (wide, head dim 64: three a CU), no run shorter than
+    // 256 keys (narrow: 128).  Narrow: keys below 512 stay whole (400 keys of 16 heads 7.4 us whole, 8.1 us in three
+    // runs), so do tiles that fill three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us whole, 38 us
+    // in three), at most 32 runs (16,000 keys of 8 KV heads 26 us, 33 us in 64); of a long cache runs of 2560 keys, which
+    // even out ragged rows (32 rows of up to 16,384 keys 257 us in two runs, 220 us in seven).
+    int64_t n;
+    if (x.wide) {
+        const int64_t want = d128 ? 512 : 1024;
+        n = std::min<int64_t>((want + work - 1) / work, kv / 256);
+    } else {
+        n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>((512 + work - 1) / work, kv / 128), 32);
+        if (kv >= 8192) n = std::max<int64_t>(n, kv / 2560);
+    }
+    n = std::max<int64_t>(1, std::min<int64_t>(n, MAX_RUNS));
     x.g.n_splits = (int)n;
     x.g.split_len = (int)(((kv + n - 1) / n + KB - 1) / KB * KB);
     if (n > 1) {
@@ -792,12 +825,8 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream) {
     hipStream_t st = (hipStream_t)hip_stream;
     const bool bf = a.cache.dtype == MTP_DTYPE_BF16;
     if (x.wide) return a.cache.head_dim == 64 ? tile_go<64>(st, a, x.g) : tile_go<128>(st, a, x.g);
-    if (x.one) {
-        if (a.cache.head_dim == 64) return bf ? rows_go<bf16_t, 64, 16>(st, a, x.g) : rows_go<float, 64, 8>(st, a, x.g);
-        return bf ? rows_go<bf16_t, 128, 8>(st, a, x.g) : rows_go<float, 128, 8>(st, a, x.g);
-    }
-    if (a.cache.head_dim == 64) return bf ? rows_go<bf16_t, 64, 4>(st, a, x.g) : rows_go<float, 64, 4>(st, a, x.g);
-    return bf ? rows_go<bf16_t, 128, 4>(st, a, x.g) : rows_go<float, 128, 4>(st, a, x.g);
+    if (a.cache.head_dim == 64) return bf ? rows_go<bf16_t, 64>(st, a, x.g) : rows_go<float, 64>(st, a, x.g);
+    return bf ? rows_go<bf16_t, 128>(st, a, x.g) : rows_go<float, 128>(st, a, x.g);
 }
 
 }  // extern "C"
