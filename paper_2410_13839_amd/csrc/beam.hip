@@ -49,8 +49,9 @@ uint64_t beam_carve(const mtp_beam_args& a, BeamWs* w) {
 }
 
 // Best first: larger value, then lower index.
-__device__ __forceinline__ bool before(float va, int ia, float vb, int ib) {
-    return (va > vb) | ((va == vb) & (ia < ib));
+// (An int, combined with & so that no step becomes a branch.)
+__device__ __forceinline__ int before(float va, int ia, float vb, int ib) {
+    return (int)(va > vb) | ((int)(va == vb) & (int)(ia < ib));
 }
 
 __device__ __forceinline__ float min_f(float a, float b) { return a < b ? a : b; }
@@ -73,7 +74,7 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        f[i] = (f[i] != f[i]) | (v0 + 64 * i == hide) ? -INFINITY : f[i];
+        f[i] = (f[i] != f[i] || v0 + 64 * i == hide) ? -INFINITY : f[i];
         top = fmaxf(top, f[i]);
     }
     // maxima of groups of lanes, at least W groups; bound: the smallest of them

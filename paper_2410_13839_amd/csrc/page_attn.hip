@@ -443,7 +443,7 @@ typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a, AttnGeo g) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_attention_args a, AttnGeo g) {
     constexpr float MSTEP = 8.0f;
     constexpr int CW = D / 8;                    // 16-byte pieces of a K row
     __shared__ __attribute__((aligned(1024))) bf16_t s_k[2][KB * D], s_v[2][KB * D];
@@ -479,10 +479,13 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
         if (a.scale == 0.f) v = u32x4_t{0, 0, 0, 0};
         q[j] = __builtin_bit_cast(bf16x8_t, v);
     }
-    int rlo, rhi, wlo, whi, alo, ahi;            // what this lane's row sees; some row of the wave; every row of it
+    // what this lane's row sees; what some row of the wave sees; what every row of the tile sees
+    int rlo, rhi, wlo, whi, tlo, thi, skip;
     sight_of(a, g, t, row, rlo, rhi);
-    sight_of(a, g, t, r0, wlo, ahi);
-    sight_of(a, g, t, r1, alo, whi);
+    sight_of(a, g, t, r0, wlo, skip);
+    sight_of(a, g, t, r1, skip, whi);
+    sight_of(a, g, t, 0, skip, thi);
+    sight_of(a, g, t, rows - 1, tlo, skip);
 
     const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
     const bf16_t* pool = (const bf16_t*)a.cache.pool + (size_t)hk * PG * D;
@@ -511,7 +514,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
             const bf16_t* base = pool + (size_t)pg * pstr;
             const int slot = in / CW, piece = (in % CW) ^ (D == 128 ? slot : (slot >> 1) & 7);
             __builtin_amdgcn_global_load_lds((gptr_t)(base + slot * D + piece * 8), (lptr_t)(&s_k[buf][step * 512]), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gptr_t)(base + vofs + in * 8), (lptr_t)(&s_v[buf][step * 512]), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr_t)(base + vofs + (in ^ ((in >> 4) & 1)) * 8), (lptr_t)(&s_v[buf][step * 512]),
+                                             16, 0, 0);
         }
         return bad;
     };
@@ -527,10 +531,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
     const int krow = (qc & 16) | ((qc & 4) << 1) | ((qc & 8) >> 1) | (qc & 3);
     const int ksw = D == 128 ? krow & 15 : (krow >> 1) & 7;
 
-    auto use = [&](int buf, int kb, int bad) {
+    // the scores of the block in buffer buf
+    auto scores = [&](int buf, f32x16_t (&s)[2]) {
         const bf16_t* K = s_k[buf] + krow * D;
-        const bf16_t* V = s_v[buf] + qc * PG + 8 * hh;
-        f32x16_t s[2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
@@ -540,18 +543,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
                 s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     *reinterpret_cast<const bf16x8_t*>(K + 32 * tt * D + ((2 * j + hh) ^ ksw) * 8), q[j], s[tt], 0, 0, 0);
         }
-        // register i of tile tt: key kb + 32 tt + 16 (i / 8) + 8 hh + i % 8, page 2 tt + i / 8 of the block
-        const bool edge = kb < alo || kb + KB > ahi || kb + KB > k1 || bad;   // uniform over the wave
-        if (edge) {
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = kb + 32 * tt + 16 * (i >> 3) + 8 * hh + (i & 7);
-                    const bool ok = key >= rlo && key < rhi && key < k1 && !(bad >> (2 * tt + (i >> 3)) & 1);
-                    s[tt][i] = ok ? s[tt][i] : -INFINITY;
-                }
-        }
+    };
+    // their probabilities; m, l and o move along
+    auto weigh = [&](const f32x16_t (&s)[2], bf16x8_t (&p)[4]) {
         float mx = -INFINITY;
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
@@ -568,7 +562,6 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
         }
         const float mm = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
-        bf16x8_t p[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             float e[8];
@@ -578,15 +571,37 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
             p[u] = __builtin_bit_cast(bf16x8_t, make_uint4(pk2(e[0], e[1]), pk2(e[2], e[3]), pk2(e[4], e[5]), pk2(e[6], e[7])));
         }
         l += sum;
-        if (!edge) {
+    };
+    // a block that every query of the tile sees whole
+    auto whole = [&](int buf) {
+        f32x16_t s[2];
+        bf16x8_t p[4];
+        scores(buf, s);
+        weigh(s, p);
+        const bf16_t* V = s_v[buf] + qc * PG + 8 * (hh ^ ((qc >> 3) & 1));
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int dt = 0; dt < D / 32; ++dt)
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        *reinterpret_cast<const bf16x8_t*>(V + u * PG * D + 32 * dt * PG), p[u], o[dt], 0, 0, 0);
-            return;
-        }
+            for (int dt = 0; dt < D / 32; ++dt)
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    *reinterpret_cast<const bf16x8_t*>(V + u * PG * D + 32 * dt * PG), p[u], o[dt], 0, 0, 0);
+    };
+    // any block
+    auto edge = [&](int buf, int kb, int bad) {
+        f32x16_t s[2];
+        bf16x8_t p[4];
+        scores(buf, s);
+        // register i of tile tt: key kb + 32 tt + 16 (i / 8) + 8 hh + i % 8, page 2 tt + i / 8 of the block
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = kb + 32 * tt + 16 * (i >> 3) + 8 * hh + (i & 7);
+                const bool ok = key >= rlo && key < rhi && key < k1 && !(bad >> (2 * tt + (i >> 3)) & 1);
+                s[tt][i] = ok ? s[tt][i] : -INFINITY;
+            }
+        weigh(s, p);
+        const bf16_t* V = s_v[buf] + qc * PG + 8 * (hh ^ ((qc >> 3) & 1));
         // values that no query sees are not multiplied (0 x infinity, 0 x NaN); among those that some see and some
         // do not, the ones that are not finite are taken out here and added below
         uint32_t odd = 0;
@@ -618,20 +633,34 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(mtp_attention_args a,
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int d = 32 * dt + 8 * (i >> 2) + 4 * hh + (i & 3);
-                        const float v = bf16_to_f32(s_v[buf][(u >> 4) * PG * D + d * PG + (u & 15)]);
+                        const float v = bf16_to_f32(s_v[buf][(u >> 4) * PG * D + d * PG + ((u & 15) ^ (d & 8))]);
                         if (sees && !(fabsf(v) < INFINITY)) o[dt][i] += v;
                     }
             }
         }
     };
 
+    // blocks [w0, w1) are seen whole by every query of the tile
+    const int w0 = max(0, (tlo - k0 + KB - 1) / KB), w1 = (min(thi, k1) - k0) / KB;
     int bad = nb > 0 ? stage(0, 0) : 0;
-    for (int j = 0; j < nb; ++j) {
-        // this wave's loads of block j have landed; all waves' have, and all are done with block j - 1's buffer
+    int j = 0;
+    // this wave's loads of block j have landed; all waves' have, and all are done with block j - 1's buffer
+    auto arrive = [&]() {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const int now = bad, kb = k0 + KB * j;
+        const int now = bad;
         if (j + 1 < nb) bad = stage((j + 1) & 1, j + 1);
-        if (wave_on && kb < whi && kb + KB > wlo) use(j & 1, kb, now);
+        return now;
+    };
+    while (j < nb) {
+        for (; j >= w0 && j < w1 && bad == 0; ++j) {
+            arrive();
+            if (wave_on) whole(j & 1);
+        }
+        if (j < nb) {
+            const int now = arrive(), kb = k0 + KB * j;
+            if (wave_on && kb < whi && kb + KB > wlo) edge(j & 1, kb, now);
+            ++j;
+        }
     }
     l = xor32_sum(l);
 
