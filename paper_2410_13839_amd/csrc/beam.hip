@@ -71,10 +71,14 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
         const int v = v0 + 64 * i;
         f[i] = v < a.vocab ? x[v] : -INFINITY;
     }
+    if (hide / CHUNK == ch) {                    // (uniform; -1 / CHUNK is 0: no index is -1)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) f[i] = v0 + 64 * i == hide ? -INFINITY : f[i];
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        f[i] = (f[i] != f[i] || v0 + 64 * i == hide) ? -INFINITY : f[i];
+        f[i] = fmaxf(f[i], -INFINITY);           // NaN: -infinity
         top = fmaxf(top, f[i]);
     }
     // maxima of groups of lanes, at least W groups; bound: the smallest of them
@@ -116,6 +120,18 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
         }
     }
     __builtin_amdgcn_wave_barrier();
+    if (n <= 64) {
+        // a lane each: its place is the number of candidates before it
+        const float2 e = buf[lane < n ? lane : 0];
+        const int id = __float_as_int(e.y);
+        int place = 0;
+        for (int k = 0; k < n; ++k) {
+            const float v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.x), k));
+            place += before(v, __builtin_amdgcn_readlane(id, k), e.x, id);
+        }
+        if (lane < n && place < W) list[place] = e;
+        return;
+    }
     float pv = INFINITY;                         // the last one taken
     int pi = -1;
     if (n <= CAP) {
@@ -186,6 +202,8 @@ struct BeamLds {
     float score[MAX_BEAMS];
     int len[MAX_BEAMS], done[MAX_BEAMS];
     float2 best[MAX_BEAMS][MAX_BEAMS];           // each beam's best logits over its chunks
+    double rank[MAX_BEAMS][MAX_BEAMS];           // its candidates, best first
+    int place[MAX_BEAMS * MAX_BEAMS];            // each candidate's place among all
 };
 
 // The request's state (the caller synchronises).
@@ -256,54 +274,52 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
         }
     }
     __syncthreads();
-    if (wave != 0) return;
-    // lane b: the head of beam b's list
-    int at = 0, tok = 0;
-    double total = -INFINITY, rank = -INFINITY;
-    int64_t flat = INT64_MAX;
-    const bool own = lane < W;
-    const double lse = own && !s.done[lane] ? s.lse[lane] : 0.0, den = own ? s.den[lane] : 1.0;
-    const float score = own ? s.score[lane] : 0.f;
-    const int dn = own ? s.done[lane] : 0;
-    // a beam without a finite score or normaliser: every candidate is -infinity, in token order
-    const bool dead = own && !dn && !(fabsf(score) < INFINITY && fabs(lse) < INFINITY);
-    auto head = [&]() {
-        flat = INT64_MAX;
-        total = rank = -INFINITY;
-        if (!own || at >= n) return;
-        if (dn) {
-            // itself first, then the tokens that it cannot take
-            tok = at == 0 ? a.eos_id : (at - 1 < a.eos_id ? at - 1 : at);
-            total = at == 0 && score < INFINITY ? (double)score : -INFINITY;     // (NaN: -infinity too)
-        } else if (dead) {
-            tok = at;
+    // the candidates, W lists of n: a finished beam's are itself and then the tokens that it cannot take, those of a
+    // beam without a finite score or normaliser all -infinity, in token order
+    auto candidate = [&](int b, int j, int& tok) {
+        double total = -INFINITY;
+        if (s.done[b]) {
+            tok = j == 0 ? a.eos_id : (j - 1 < a.eos_id ? j - 1 : j);
+            if (j == 0 && s.score[b] < INFINITY) total = (double)s.score[b];     // (NaN: -infinity too)
+        } else if (!(fabsf(s.score[b]) < INFINITY && fabs(s.lse[b]) < INFINITY)) {
+            tok = j;
         } else {
-            const float2 e = s.best[lane][at];
-            tok = __float_as_int(e.y);
-            total = (double)score + ((double)e.x - lse);
+            tok = __float_as_int(s.best[b][j].y);
+            total = (double)s.score[b] + ((double)s.best[b][j].x - s.lse[b]);
         }
-        rank = total / den;
-        flat = (int64_t)lane * a.vocab + tok;
+        return total;
     };
-    head();
-    for (int k = 0; k < W; ++k) {
-        double br = rank;
-        long long bf = flat;
-        for (int o = 1; o < W; o <<= 1) {
-            const double orr = __shfl_xor(br, o);
-            const long long of = __shfl_xor(bf, o);
-            if (orr > br || (orr == br && of < bf)) { br = orr; bf = of; }
+    for (int c = threadIdx.x; c < W * n; c += 64 * NW) {
+        const int b = c / n, j = c - b * n;
+        int tok;
+        s.rank[b][j] = candidate(b, j, tok) / s.den[b];
+        s.place[c] = j;                          // those of its own beam before it
+    }
+    __syncthreads();
+    // a candidate's place: how many of every other beam's come before it (equal ones: those of the earlier beam)
+    for (int p = threadIdx.x; p < W * n * W; p += 64 * NW) {
+        const int c = p / W, o = p - c * W, b = c / n, j = c - b * n;
+        if (o == b) continue;
+        const double mine = s.rank[b][j];
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            const double r2 = s.rank[o][mid];
+            if (r2 > mine || (r2 == mine && o < b)) lo = mid + 1; else hi = mid;
         }
-        if (own && flat == bf) {                         // one lane: the head that is taken
-            const int o = r * W + k;
-            a.out_score[o] = (float)total;
-            a.out_len[o] = s.len[lane];
-            a.out_done[o] = dn | (tok == a.eos_id ? 1 : 0);
-            a.out_parent[o] = r * W + lane;
-            a.out_token[o] = tok;
-            ++at;
-            head();
-        }
+        if (lo) atomicAdd(&s.place[c], lo);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < W * n; c += 64 * NW) {
+        if (s.place[c] >= W) continue;
+        const int b = c / n, j = c - b * n, o = r * W + s.place[c];
+        int tok;
+        const double total = candidate(b, j, tok);
+        a.out_score[o] = (float)total;
+        a.out_len[o] = s.len[b];
+        a.out_done[o] = s.done[b] | (tok == a.eos_id ? 1 : 0);
+        a.out_parent[o] = r * W + b;
+        a.out_token[o] = tok;
     }
 }
 

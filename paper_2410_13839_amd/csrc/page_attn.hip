@@ -535,14 +535,22 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_att
     auto scores = [&](int buf, f32x16_t (&s)[2]) {
         const bf16_t* K = s_k[buf] + krow * D;
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j)
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
                 s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     *reinterpret_cast<const bf16x8_t*>(K + 32 * tt * D + ((2 * j + hh) ^ ksw) * 8), q[j], s[tt], 0, 0, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < D / 8 - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     };
     // their probabilities; m, l and o move along
     auto weigh = [&](const f32x16_t (&s)[2], bf16x8_t (&p)[4]) {
@@ -585,6 +593,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_att
             for (int dt = 0; dt < D / 32; ++dt)
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     *reinterpret_cast<const bf16x8_t*>(V + u * PG * D + 32 * dt * PG), p[u], o[dt], 0, 0, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < D / 8 - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     };
     // any block
     auto edge = [&](int buf, int kb, int bad) {
@@ -688,71 +703,105 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_att
     }
 }
 
-// Joins a tile's runs: one wave per query row.  The runs' weights exp2(m_s - m)
-// once (lane i: runs i, i + 64, ...), then every group of D / 4 lanes takes
-// runs in turn, its loads independent of each other.
-constexpr int JW = 4;                            // waves (rows) of a workgroup
+// Joins a tile's runs: one wave per JR query rows, whose loads are in flight
+// together.  The runs' weights exp2(m_s - m) once (lane i: runs i, i + 64, ...),
+// then every group of D / 4 lanes takes runs in turn.
+constexpr int JW = 4;                            // waves of a workgroup
 
-template <typename T, int D, int RT>
+constexpr int JFEW = 4;                          // runs up to which a wave takes four rows
+
+template <typename T, int D, int RT, int JR>
 __global__ __launch_bounds__(64 * JW) void attn_join_kernel(mtp_attention_args a, AttnGeo g) {
+    constexpr int NL = JR == 1 ? MAX_RUNS / 64 : 1;    // runs of a lane
     constexpr int LD = D / 4, SG = 64 / LD;      // lanes of a row's dimensions, runs at a time
-    __shared__ float s_w[JW][MAX_RUNS];
+    __shared__ float s_w[JW][JR][64 * NL];
     const int H = a.cache.n_kv_heads, HB = H * g.hb, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb, qr = blockIdx.y * JW + wave;
+    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb, q0 = (blockIdx.y * JW + wave) * JR;
     const AttnTile t = find_tile(a, g, tile);
-    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs, heads = min(g.gs, group - h0);
-    if (qr >= t.nt * g.gs || qr % g.gs >= heads) return;
+    const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs, heads = min(g.gs, group - h0), rows = t.nt * g.gs;
+    if (q0 >= rows) return;
     int k0, k1;
     const int live = runs_of(g, t, 0, k0, k1);
     if (live <= 1) return;
-    const size_t slot = (size_t)blockIdx.x * g.n_splits * RT + qr;
-    // (a run that the row sees nothing of has m = -infinity and l = 0; one whose scores are not numbers l = NaN)
-    float2 x[MAX_RUNS / 64];
-    float m = -INFINITY, l = 0.f;
+    const size_t slot = (size_t)blockIdx.x * g.n_splits * RT + q0;
+    // (a run that the row sees nothing of has m = -infinity and l = 0; one whose scores are not numbers l = NaN; rows
+    // that do not exist read the first one's)
+    float2 x[JR][NL];
+    float m[JR], l[JR];
 #pragma unroll
-    for (int i = 0; i < MAX_RUNS / 64; ++i) {
-        x[i] = make_float2(-INFINITY, 0.f);
-        if (64 * i + lane < live) x[i] = g.ml[slot + (size_t)(64 * i + lane) * RT];
-        m = fmaxf(m, x[i].x);
-    }
-    m = wave_max64(m);
+    for (int k = 0; k < JR; ++k)
 #pragma unroll
-    for (int i = 0; i < MAX_RUNS / 64; ++i) {
-        const float w = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[i].x - m);
-        l += x[i].x == -INFINITY ? x[i].y : w * x[i].y;
-        s_w[wave][64 * i + lane] = w;
+        for (int i = 0; i < NL; ++i) {
+            x[k][i] = make_float2(-INFINITY, 0.f);
+            if (64 * i + lane < live) x[k][i] = g.ml[slot + (q0 + k < rows ? k : 0) + (size_t)(64 * i + lane) * RT];
+        }
+#pragma unroll
+    for (int k = 0; k < JR; ++k) {
+        m[k] = -INFINITY;
+        l[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) m[k] = fmaxf(m[k], x[k][i].x);
+        m[k] = wave_max64(m[k]);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const float w = x[k][i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[k][i].x - m[k]);
+            l[k] += x[k][i].x == -INFINITY ? x[k][i].y : w * x[k][i].y;
+            s_w[wave][k][64 * i + lane] = w;
+        }
+        l[k] = wave_sum64(l[k]);
     }
-    l = wave_sum64(l);
     __builtin_amdgcn_wave_barrier();
     const int sg = lane / LD, d = (lane - sg * LD) * 4;
-    f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
+    f32x4_t v[JR];
+#pragma unroll
+    for (int k = 0; k < JR; ++k) v[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll JR == 1 ? 8 : 2
     for (int s = sg; s < live; s += SG) {
-        const float w = s_w[wave][s];
-        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(&g.acc[(slot + (size_t)s * RT) * D + d]);
-        if (w != 0.f) v += o * w;
+#pragma unroll
+        for (int k = 0; k < JR; ++k) {
+            const float w = s_w[wave][k][s];
+            const f32x4_t o =
+                *reinterpret_cast<const f32x4_t*>(&g.acc[(slot + (q0 + k < rows ? k : 0) + (size_t)s * RT) * D + d]);
+            if (w != 0.f) v[k] += o * w;
+        }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (LD == 16) v[e] = xor16_sum(v[e]);
-        v[e] = xor32_sum(v[e]);
+    for (int k = 0; k < JR; ++k) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (LD == 16) v[k][e] = xor16_sum(v[k][e]);
+            v[k][e] = xor32_sum(v[k][e]);
+        }
+        const int qr = q0 + k;
+        if (sg != 0 || qr >= rows || qr % g.gs >= heads) continue;
+        const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
+        T* op = (T*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + d;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<uint2*>(op) = make_uint2(pk2(v[k][0] * inv, v[k][1] * inv), pk2(v[k][2] * inv, v[k][3] * inv));
+        else
+            *reinterpret_cast<f32x4_t*>(op) = v[k] * inv;
     }
-    if (sg != 0) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* op = (T*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + d;
-    if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<uint2*>(op) = make_uint2(pk2(v[0] * inv, v[1] * inv), pk2(v[2] * inv, v[3] * inv));
-    else
-        *reinterpret_cast<f32x4_t*>(op) = v * inv;
 }
 
 // ------------------------------------------------------------------- launches
+// (Four rows a wave where there are few runs: two runs of 488 wide tiles 28 us with one row a wave, JOIN4; many
+// runs of few tiles are faster with a row each: 11 runs of 48 wide tiles, the whole call 51.5 and 41 us.)
+template <typename T, int D, int RT>
+void join_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g, unsigned work) {
+    if (g.n_splits <= 1) return;
+    const int rows = g.tt * g.gs;
+    if (g.n_splits <= JFEW)
+        hipLaunchKernelGGL((attn_join_kernel<T, D, RT, 4>), dim3(work, (rows + 4 * JW - 1) / (4 * JW)), dim3(64 * JW), 0, st, a, g);
+    else
+        hipLaunchKernelGGL((attn_join_kernel<T, D, RT, 1>), dim3(work, (rows + JW - 1) / JW), dim3(64 * JW), 0, st, a, g);
+}
+
 template <typename T, int D>
 int rows_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
     hipLaunchKernelGGL((attn_rows_kernel<T, D>), dim3(work, g.n_splits), dim3(64 * NW), 0, st, a, g);
-    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<T, D, 16>), dim3(work, (g.tt * g.gs + JW - 1) / JW), dim3(64 * JW), 0, st, a, g);
+    join_go<T, D, 16>(st, a, g, work);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
 
@@ -760,7 +809,7 @@ template <int D>
 int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
     hipLaunchKernelGGL((attn_tile_kernel<D>), dim3((work * g.n_splits + 7) / 8 * 8), dim3(256), 0, st, a, g);
-    if (g.n_splits > 1) hipLaunchKernelGGL((attn_join_kernel<bf16_t, D, TR>), dim3(work, (g.tt * g.gs + JW - 1) / JW), dim3(64 * JW), 0, st, a, g);
+    join_go<bf16_t, D, TR>(st, a, g, work);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
 
