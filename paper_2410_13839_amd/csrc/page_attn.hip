@@ -105,12 +105,23 @@ __device__ __forceinline__ void sight_of(const mtp_attention_args& a, const Attn
 
 __device__ __forceinline__ uint32_t pk2(float a, float b) { return bf16x2_bits(a, b); }
 
-// Two bf16 with those that are not finite set to zero; `seen` collects whether
-// there were any.
-__device__ __forceinline__ uint32_t finite2(uint32_t v, uint32_t& seen) {
+// Two bf16 with those that are not finite set to zero.
+__device__ __forceinline__ uint32_t finite2(uint32_t v) {
     const bool lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
-    seen |= (lo | hi) ? 1u : 0u;
     return v & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+}
+// The larger magnitudes, halves apart, of two pairs of bf16 bits (`most`
+// without signs); a half of 0x7f80 or more is not finite.
+__device__ __forceinline__ uint32_t larger2(uint32_t most, uint32_t v) {
+    typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, most),
+                                                                  __builtin_bit_cast(u16x2_t, v & 0x7fff7fffu)));
+}
+__device__ __forceinline__ bool odd2(uint32_t most) { return (most & 0xffffu) >= 0x7f80u || (most >> 16) >= 0x7f80u; }
+
+// Bits of keys y and y + 1 that lie in [lo, hi).
+__device__ __forceinline__ uint32_t inside2(int y, int lo, int hi) {
+    return (y >= lo && y < hi ? 0xffffu : 0u) | (y + 1 >= lo && y + 1 < hi ? 0xffff0000u : 0u);
 }
 
 // ------------------------------------------------------------ few query rows
@@ -203,6 +214,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
     int alo, ahi, unused;
     sight_of(a, g, t, rows - 1, alo, unused);
     sight_of(a, g, t, 0, unused, ahi);
+    const bool mixed = alo != t.lo || ahi != t.hi;       // some keys of the tile are seen by some of its queries only
 
     const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
     const T* pool = (const T*)a.cache.pool + (size_t)hk * PG * D;
@@ -268,40 +280,42 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
             return sizeof(T) == 2 ? !(b >> (gr >> 1) & 1) : !(b >> (u >> 2) & 1);
         };
         const bool edge = kb < alo || kb + 32 > ahi || kb + 32 > k1 || b;    // uniform
-        uint32_t odd = 0;
+        bool odd = false;
         if (edge) {
+            const int slo = max(rlo, t.lo), shi = min(rhi, k1);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int key = key_of(u);
-                s[u] = key >= rlo && key < rhi && key < k1 && there(u) ? s[u] : -INFINITY;
-            }
-            // values that no query sees are not multiplied (0 x infinity, 0 x NaN); among those that some see and
-            // some do not, the ones that are not finite are taken out here and added below
+            for (int u = 0; u < 8; ++u) s[u] = key_of(u) >= slo && key_of(u) < shi && there(u) ? s[u] : -INFINITY;
+            // values that no query sees are not multiplied (0 x infinity, 0 x NaN); among those that some see and some
+            // do not, the ones that are not finite are taken out here and added below
             if constexpr (sizeof(T) == 2) {
-                uint32_t in[4];
+                uint32_t in[4], most = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int y0 = kb + 8 * gr + 2 * j, y1 = y0 + 1;
-                    in[j] = there(0) ? (y0 >= t.lo && y0 < k1 ? 0xffffu : 0u) | (y1 >= t.lo && y1 < k1 ? 0xffff0000u : 0u) : 0u;
-                }
+                for (int j = 0; j < 4; ++j) in[j] = there(0) ? inside2(kb + 8 * gr + 2 * j, t.lo, k1) : 0u;
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
                     uint4& v = x.v[dt];
-                    v = make_uint4(finite2(v.x & in[0], odd), finite2(v.y & in[1], odd), finite2(v.z & in[2], odd),
-                                   finite2(v.w & in[3], odd));
+                    v = make_uint4(v.x & in[0], v.y & in[1], v.z & in[2], v.w & in[3]);
+                    most = larger2(larger2(larger2(larger2(most, v.x), v.y), v.z), v.w);
+                }
+                odd = mixed && odd2(most);
+                if (__any(odd)) {
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) {
+                        uint4& v = x.v[dt];
+                        v = make_uint4(finite2(v.x), finite2(v.y), finite2(v.z), finite2(v.w));
+                    }
                 }
             } else {
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const int key = key_of(u);
-                    const bool in = key >= t.lo && key < k1 && there(u);
+                    const bool in = key_of(u) >= t.lo && key_of(u) < k1 && there(u);
 #pragma unroll
                     for (int i2 = 0; i2 < D / 64; ++i2) {
                         float* v = reinterpret_cast<float*>(&x.v[u >> 2][u & 3][i2]);
 #pragma unroll
                         for (int d = 0; d < 4; ++d) {
-                            const bool fin = fabsf(v[d]) < INFINITY;
-                            odd |= in && !fin ? 1u : 0u;
+                            const bool fin = !mixed || fabsf(v[d]) < INFINITY;
+                            odd |= in && !fin;
                             v[d] = in && fin ? v[d] : 0.f;
                         }
                     }
@@ -486,6 +500,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_att
     sight_of(a, g, t, r1, skip, whi);
     sight_of(a, g, t, 0, skip, thi);
     sight_of(a, g, t, rows - 1, tlo, skip);
+    const bool mixed = tlo != t.lo || thi != t.hi;       // some keys of the tile are seen by some of its queries only
 
     const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
     const bf16_t* pool = (const bf16_t*)a.cache.pool + (size_t)hk * PG * D;
@@ -607,37 +622,50 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_att
         bf16x8_t p[4];
         scores(buf, s);
         // register i of tile tt: key kb + 32 tt + 16 (i / 8) + 8 hh + i % 8, page 2 tt + i / 8 of the block
+        const int slo = max(rlo, t.lo) - (kb + 8 * hh);
+        const unsigned span = max(0, min(rhi, k1) - max(rlo, t.lo));
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = kb + 32 * tt + 16 * (i >> 3) + 8 * hh + (i & 7);
-                const bool ok = key >= rlo && key < rhi && key < k1 && !(bad >> (2 * tt + (i >> 3)) & 1);
-                s[tt][i] = ok ? s[tt][i] : -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i)
+                s[tt][i] = (unsigned)(32 * tt + 16 * (i >> 3) + (i & 7) - slo) < span ? s[tt][i] : -INFINITY;
+        if (bad) {
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[tt][i] = bad >> (2 * tt + (i >> 3)) & 1 ? -INFINITY : s[tt][i];
+        }
         weigh(s, p);
         const bf16_t* V = s_v[buf] + qc * PG + 8 * (hh ^ ((qc >> 3) & 1));
         // values that no query sees are not multiplied (0 x infinity, 0 x NaN); among those that some see and some
         // do not, the ones that are not finite are taken out here and added below
-        uint32_t odd = 0;
+        bool odd = false;
+        if (mixed) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(V + u * PG * D + 32 * dt * PG);
+                    most = larger2(larger2(larger2(larger2(most, v.x), v.y), v.z), v.w);
+                }
+            odd = odd2(most);                    // (of keys outside [t.lo, k1) too: those come to nothing below)
+        }
+        const bool any_odd = __any(odd);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             uint32_t in[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int y0 = kb + 16 * u + 8 * hh + 2 * j, y1 = y0 + 1;
-                in[j] = bad >> u & 1 ? 0u
-                                     : (y0 >= t.lo && y0 < k1 ? 0xffffu : 0u) | (y1 >= t.lo && y1 < k1 ? 0xffff0000u : 0u);
-            }
+            for (int j = 0; j < 4; ++j) in[j] = bad >> u & 1 ? 0u : inside2(kb + 16 * u + 8 * hh + 2 * j, t.lo, k1);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt) {
                 uint4 v = *reinterpret_cast<const uint4*>(V + u * PG * D + 32 * dt * PG);
-                v = make_uint4(finite2(v.x & in[0], odd), finite2(v.y & in[1], odd), finite2(v.z & in[2], odd),
-                               finite2(v.w & in[3], odd));
+                v = make_uint4(v.x & in[0], v.y & in[1], v.z & in[2], v.w & in[3]);
+                if (any_odd) v = make_uint4(finite2(v.x), finite2(v.y), finite2(v.z), finite2(v.w));
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[u], o[dt], 0, 0, 0);
             }
         }
-        if (__any(odd)) {
+        if (any_odd) {
             // an infinite or NaN value reaches exactly the queries that see it
             for (int u = 0; u < KB; ++u) {
                 const int key = kb + u;
