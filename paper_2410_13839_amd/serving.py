@@ -59,8 +59,14 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _i32(x: int, name: str) -> int:
+    if not -(1 << 31) <= x < 1 << 31:            # (ctypes would drop the upper bits)
+        raise ValueError(f"{name}: {x} does not fit 32 bits")
+    return x
+
+
 def _ints(t: torch.Tensor, name: str, shape, device) -> int:
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device}, "
                          f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -129,6 +135,8 @@ def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num
     dev = _device(length, "length")
     _need(table.dim() == 2 and length.dim() == 1, "length: [rows]; table: [rows, max_pages]")
     n, m = table.shape
+    _need(0 <= max_tokens < 1 << 31 and 0 < num_pages < 1 << 27 and m < 1 << 31,
+          "max_tokens in [0, 2^31), num_pages in [1, 2^27), max_pages in 32 bits")
     p_len, p_add = _ints(length, "length", (n,), dev), _ints(add, "add", (n,), dev)
     p_in = _ints(table, "table", (n, m), dev)
     p_par = None if parent is None else _ints(parent, "parent", (n,), dev)
@@ -149,7 +157,9 @@ def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num
         tok.fill_(-1)
     else:
         _launch(_b.mtp_pages_plan, args, dev)
-    return PagePlan(new, small[3 * n:4 * n + 1], small[2 * n:3 * n], tok[0], tok[1], small[:2 * n].view(n, 2), small[4 * n + 1:])
+    copies, kv_len, row_start, status = small.split((2 * n, n, n + 1, 4))
+    slots, positions = tok.unbind(0)
+    return PagePlan(new, row_start, kv_len, slots, positions, copies.view(n, 2), status)
 
 
 def write_pages(pool: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
@@ -194,10 +204,13 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
     n, m = table.shape
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    _need(out.shape == q.shape, "out: q's shape")
-    os = _rows(out, "out", pool, dim)
-    args = _b.mtp_attention_args(cache, n, m, q.shape[0], q.shape[1], _b.MTP_ATTN_CAUSAL if causal else _b.MTP_ATTN_FULL,
-                                 window, max_kv, dim ** -0.5 if scale is None else scale,
+        os = q.shape[1] * dim
+    else:
+        _need(out.shape == q.shape, "out: q's shape")
+        os = _rows(out, "out", pool, dim)
+    args = _b.mtp_attention_args(cache, n, _i32(m, "max_pages"), _i32(q.shape[0], "tokens"), q.shape[1],
+                                 _b.MTP_ATTN_CAUSAL if causal else _b.MTP_ATTN_FULL, _i32(window, "window"),
+                                 _i32(max_kv, "max_kv"), dim ** -0.5 if scale is None else scale,
                                  _ints(table, "table", (n, m), dev), _ints(row_start, "row_start", (n + 1,), dev),
                                  _ints(kv_len, "kv_len", (n,), dev), q.data_ptr(), out.data_ptr(), qs, os, None, 0)
     ws = _workspace(_b.mtp_pages_attention_workspace_size, args, dev)
@@ -221,7 +234,7 @@ def select_beams(logits: torch.Tensor, score: torch.Tensor, length: torch.Tensor
           "score: contiguous float32 [requests, beams] on the logits' device")
     new = torch.empty((5, r, w), dtype=torch.int32, device=dev)
     base, step = new.data_ptr(), 4 * r * w
-    args = _b.mtp_beam_args(r, w, v, eos_id, eos_min, alpha, logits.data_ptr(), ld, score.data_ptr(),
+    args = _b.mtp_beam_args(_i32(r, "requests"), w, _i32(v, "vocab"), _i32(eos_id, "eos_id"), _i32(eos_min, "eos_min"), alpha, logits.data_ptr(), ld, score.data_ptr(),
                             _ints(length, "length", (r, w), dev), _ints(done, "done", (r, w), dev), base, base + step,
                             base + 2 * step, base + 3 * step, base + 4 * step, None, 0)
     ws = _workspace(_b.mtp_beam_select_workspace_size, args, dev)
