@@ -169,32 +169,36 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
     }
 }
 
-// One wave: the n best of `entries` <= 64 N (logit, index bits) pairs.
+// One wave's (logit, index bits) pairs, at most 64 N, and the n best of them.
 template <int N>
-__device__ __forceinline__ void best_of_list(const float2* list, int entries, int n, float2* out) {
-    const int lane = threadIdx.x & 63;
+struct BeamList {
     float f[N];
     int id[N];
+    __device__ __forceinline__ void load(const float2* list, int entries) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const bool in = 64 * i + lane < entries;
-        const float2 e = list[in ? 64 * i + lane : 0];
-        f[i] = in ? e.x : -INFINITY;
-        id[i] = in ? __float_as_int(e.y) : 0x7fffffff;
+        for (int i = 0; i < N; ++i) {
+            const bool in = 64 * i + lane < entries;
+            const float2 e = list[in ? 64 * i + lane : 0];
+            f[i] = in ? e.x : -INFINITY;
+            id[i] = in ? __float_as_int(e.y) : 0x7fffffff;
+        }
     }
-    float pv = INFINITY;
-    int pi = -1;
-    for (int w = 0; w < n; ++w) {
-        float bv = -INFINITY;
-        int bi = 0x7fffffff;
+    __device__ __forceinline__ void best(int n, float2* out) const {
+        float pv = INFINITY;
+        int pi = -1;
+        for (int w = 0; w < n; ++w) {
+            float bv = -INFINITY;
+            int bi = 0x7fffffff;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (before(pv, pi, f[i], id[i]) & before(f[i], id[i], bv, bi)) { bv = f[i]; bi = id[i]; }
-        wave_argmax_uniform(bv, bi);
-        if (lane == 0) out[w] = make_float2(bv, __int_as_float(bi));
-        pv = bv; pi = bi;
+            for (int i = 0; i < N; ++i)
+                if (before(pv, pi, f[i], id[i]) & before(f[i], id[i], bv, bi)) { bv = f[i]; bi = id[i]; }
+            wave_argmax_uniform(bv, bi);
+            if ((threadIdx.x & 63) == 0) out[w] = make_float2(bv, __int_as_float(bi));
+            pv = bv; pi = bi;
+        }
     }
-}
+};
 
 // The waves' own scratch.
 struct BeamLds {
@@ -223,6 +227,10 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.beams, n = min(W, a.vocab);
     for (int b = wave; b < W; b += NW) {
         if (s.done[b]) continue;                 // uniform over the wave
+        const float2* bl = list + (size_t)b * chunks * W;
+        const int entries = chunks * W;
+        BeamList<4> few;                         // (its loads in flight during the sums below)
+        if (chunks > 1 && (FEW || entries <= 64 * 4)) few.load(bl, entries);
         const float* bm = max + (size_t)b * chunks;
         const double* bs = sum + (size_t)b * chunks;
         float m = -INFINITY;
@@ -232,18 +240,18 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
         for (int i = lane; i < chunks; i += 64) t += bs[i] * exp((double)bm[i] - (double)m);
         for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
         if (lane == 0) s.lse[b] = (double)m + log(t);
-        const float2* bl = list + (size_t)b * chunks * W;
         if (chunks == 1) {
             if (lane < n) s.best[b][lane] = bl[lane];
             continue;
         }
-        const int entries = chunks * W;
         if (FEW || entries <= 64 * 4) {
-            best_of_list<4>(bl, entries, n, s.best[b]);
+            few.best(n, s.best[b]);
             continue;
         }
         if (entries <= 64 * NV) {
-            best_of_list<NV>(bl, entries, n, s.best[b]);
+            BeamList<NV> many;
+            many.load(bl, entries);
+            many.best(n, s.best[b]);
             continue;
         }
         // lane i: the heads of the lists of chunks i, i + 64, ... (the best of them, advanced past what was taken)
