@@ -249,6 +249,28 @@ int mtp_get_lattice(mtp_ctx* ctx, int32_t* cand, float* ehat, float* delta,
  * for bad arguments, with nothing changed. */
 int mtp_force_tokens(mtp_ctx* ctx, const int32_t* tokens, const int32_t* count);
 
+/* Beam search: replaces what the last decode step, which must have used one
+ * head (K = 1), emitted.  The batch is B / beams requests of `beams` rows each
+ * (rows r * beams .. of request r; prefill gives each the request's prompt),
+ * and the rows' next beams are chosen over beams x vocabulary by
+ * mtp_beam_select's rule on the step's logits, with the context's eos_id and
+ * eos_min, a row's generated count as its length and its accumulated score,
+ * which starts at 0 for a request's first row and -infinity for the others at
+ * the first call after a prefill.  Row c then continues row parent[c]: its
+ * state, emitted history and cached keys are the parent's (full pages shared,
+ * a partly filled last page copied), and the chosen token is its pending chunk;
+ * EOS or the budget ends it, and an ended row that is kept stays as it is.
+ * out_tokens[B] (-1 for an ended row), out_parent[B] and out_score[B] (the
+ * sum of the row's log probabilities) are host arrays, any of them NULL; with
+ * all three NULL the call does not synchronise.  beams is 1..32, divides B and
+ * stays the same until the next prefill; alpha in [0, 32]; the rows of a
+ * request need prompts of the same lengths (MTP_EINVAL otherwise).  MTP_ESTATE
+ * unless a decode step with K = 1 ran since the last prefill and the last call
+ * of this kind.  mtp_force_tokens may follow; it leaves the scores as they
+ * are. */
+int mtp_beam_advance(mtp_ctx* ctx, int beams, float alpha, int32_t* out_tokens, int32_t* out_parent,
+                     float* out_score);
+
 /* Selection options for the following decode steps (paper Sec. 3.3, Fig. 2).
  * lattice MTP_LATTICE_OWN (default): position t's states are head t's own
  * top_k.  MTP_LATTICE_UNION: every position's states are the m <= K*top_k

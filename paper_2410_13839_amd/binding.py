@@ -35,7 +35,7 @@ EXPORTED = ["mtp_query_sizes", "mtp_weight_offset", "mtp_create", "mtp_prefill",
             "mtp_decode_step_async", "mtp_get_logits", "mtp_get_lattice", "mtp_force_tokens", "mtp_get_seq_state",
             "mtp_get_tokens",
             "mtp_profile_replay", "mtp_reset", "mtp_destroy", "mtp_last_error", "mtp_strerror",
-            "mtp_set_selection", "mtp_get_union_lattice", "mtp_set_sampling", "mtp_get_uniforms",
+            "mtp_beam_advance", "mtp_set_selection", "mtp_get_union_lattice", "mtp_set_sampling", "mtp_get_uniforms",
             "mtp_q_workspace_size", "mtp_q_count", "mtp_q_count_noalloc", "mtp_q_normalize",
             "mtp_nar_prepare", "mtp_nar_run", "mtp_nar_get_codes", "mtp_nar_get_logits",
             "mtp_pages_plan_workspace_size", "mtp_pages_plan", "mtp_pages_write", "mtp_pages_copy",
@@ -116,6 +116,7 @@ _lib.mtp_decode_step_async.argtypes = [_ctx, ctypes.c_int, ctypes.c_int, ctypes.
 _lib.mtp_get_logits.argtypes = [_ctx, _f32p]
 _lib.mtp_get_lattice.argtypes = [_ctx, _i32p, _f32p, _f32p, _i32p, _i32p]
 _lib.mtp_force_tokens.argtypes = [_ctx, _i32p, _i32p]
+_lib.mtp_beam_advance.argtypes = [_ctx, ctypes.c_int, ctypes.c_float, _i32p, _i32p, _f32p]
 _lib.mtp_set_selection.argtypes = [_ctx, ctypes.c_int, ctypes.c_int]
 _lib.mtp_get_union_lattice.argtypes = [_ctx, _i32p, _i32p, _f32p, _f32p, _i32p, _i32p]
 _lib.mtp_set_sampling.argtypes = [_ctx, ctypes.c_int, ctypes.c_float, ctypes.c_uint64]
@@ -250,6 +251,14 @@ def mtp_get_logits(ctx, B: int, K: int, V: int) -> np.ndarray:
     out = np.zeros((B, K, V), np.float32)
     _check(_lib.mtp_get_logits(ctx, out.ctypes.data_as(_f32p)), ctx, "mtp_get_logits")
     return out
+
+
+def mtp_beam_advance(ctx, B: int, beams: int, alpha: float = 0.0) -> Dict[str, np.ndarray]:
+    """tokens and parent int32 [B], score float32 [B] of the chosen beams."""
+    tok, par, score = np.zeros(B, np.int32), np.zeros(B, np.int32), np.zeros(B, np.float32)
+    _check(_lib.mtp_beam_advance(ctx, beams, alpha, tok.ctypes.data_as(_i32p), par.ctypes.data_as(_i32p),
+                                 score.ctypes.data_as(_f32p)), ctx, "mtp_beam_advance")
+    return dict(tokens=tok, parent=par, score=score)
 
 
 def mtp_set_selection(ctx, lattice: int, anchored: bool) -> None:
@@ -525,6 +534,12 @@ class Session:
 
     def step_async(self, K: int, top_k: int) -> None:
         mtp_decode_step_async(self.ctx, K, top_k)
+
+    def beam_step(self, beams: int, alpha: float = 0.0) -> Dict[str, np.ndarray]:
+        """One step of beam search: a decode step of the first head, then the
+        choice over beams x vocabulary (rows r * beams .. are request r's)."""
+        self.step(1, 1)
+        return mtp_beam_advance(self.ctx, self.B, beams, alpha)
 
     def logits(self, K: int) -> np.ndarray:
         return mtp_get_logits(self.ctx, self.B, K, self.cfg.vocab)

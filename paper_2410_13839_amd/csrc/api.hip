@@ -131,7 +131,7 @@ struct WsLayout {
     uint64_t rows, ids, tiles, last_row, state, btab, h, q, qh, u, attn, ffn, part, apart, kvnew, fsync, ffs, hz, z, logits,
         cand, ehat,
         u_states, u_m, u_ehat, u_delta, u_psi, smp_cfg, smp_u, codes, tgt_rows, nar_logits,
-        delta, psi, slots, out_tok, out_cnt, hist, total;
+        delta, psi, slots, out_tok, out_cnt, hist, bm_rows, bm_state, bm_hist, bm_tab, bm_plan, bm_plan_bytes, total;
     int64_t m_pre, m_dec, m_max, max_tiles, max_splits, maxp, num_pages;
     int act_bytes;
 };
@@ -203,6 +203,19 @@ WsLayout ws_layout(const mtp_config& c) {
     w.codes = take(nar ? w.m_pre * 8 * 4 : 0);                         // NAR: codec codes per row
     w.tgt_rows = take(nar ? w.m_pre * 4 : 0);                         // NAR: rows of the target positions
     w.nar_logits = take(nar ? (uint64_t)KH * w.m_pre * (V - 1) * 4 : 0);   // NAR: every stage's logits
+    // beam search (mtp_beam_advance): eight arrays of a word per row, the
+    // plan's small outputs, the rows' next state, history and table
+    w.bm_rows = take(nar ? 0 : (uint64_t)(8 * B + (B + 1) + 3 * B + 4) * 4);
+    w.bm_state = take(nar ? 0 : B * sizeof(SeqState));
+    w.bm_hist = take(nar ? 0 : B * (int64_t)c.max_new * 4);
+    w.bm_tab = take(nar ? 0 : B * w.maxp * 4);
+    w.bm_plan_bytes = 0;
+    if (!nar) {
+        mtp_plan_args pa{};
+        pa.n_rows = (int32_t)B; pa.max_pages = (int32_t)w.maxp; pa.num_pages = (int32_t)w.num_pages;
+        (void)mtp_pages_plan_workspace_size(&pa, &w.bm_plan_bytes);   // (a pool it refuses is refused by the call)
+    }
+    w.bm_plan = take(w.bm_plan_bytes);
     w.total = o;
     return w;
 }
@@ -260,6 +273,10 @@ struct mtp_ctx {
     StepLaunches* recording = nullptr;
     StepKey last_key{};
     bool has_last = false;
+    // beam search: the last step (of one head) awaits its choice; beams per
+    // request since the search began, 0 before
+    bool beam_ready = false;
+    int beams = 0;
 
     char* W() const { return (char*)buf.weights; }
     char* WS() const { return (char*)buf.workspace; }
@@ -848,6 +865,7 @@ int step_common(mtp_ctx* c, int K, int top_k) {
         return r;
     };
     c->has_last = false;
+    c->beam_ready = false;
     int rc;
     if (!use_graph) {
         rc = record();
@@ -872,6 +890,7 @@ int step_common(mtp_ctx* c, int K, int top_k) {
     if (rc == MTP_OK) {
         c->q_pad = K;
         c->last_K = K;
+        c->beam_ready = K == 1;
         c->last_topk = top_k;
         c->last_lattice = c->lattice;
         c->last_sample = c->sample;
@@ -1042,6 +1061,8 @@ int mtp_prefill(mtp_ctx* c, int B, const int32_t* phon, const int32_t* phon_len,
     }
     c->q_pad = 0;
     c->prefilled = true;
+    c->beam_ready = false;
+    c->beams = 0;
     c->n_pre_rows = rows;
     c->n_pre_tiles = n_tiles;
     return MTP_OK;
@@ -1174,6 +1195,67 @@ int mtp_force_tokens(mtp_ctx* c, const int32_t* tokens, const int32_t* count) {
     HIPCHK(c, hipMemcpyAsync(c->WS() + c->ws.out_cnt, out_cnt.data(), B * 4, hipMemcpyHostToDevice, st), "counts");
     HIPCHK(c, hipStreamSynchronize(st), "sync");
     return MTP_OK;
+}
+
+int mtp_beam_advance(mtp_ctx* c, int beams, float alpha, int32_t* out_tokens, int32_t* out_parent, float* out_score) {
+    if (!c) return MTP_EINVAL;
+    const mtp_config& cf = c->cfg;
+    if (is_nar(cf)) { c->err = "a NAR context has no decode steps"; return MTP_EINVAL; }
+    if (!c->prefilled || !c->beam_ready) { c->err = "no decode step of one head whose choice is open"; return MTP_ESTATE; }
+    const int B = c->B;
+    if (beams < 1 || beams > 32 || B % beams) { c->err = "beams must be in 1..32 and divide the batch"; return MTP_EINVAL; }
+    if (!(alpha >= 0.f) || alpha > 32.f) { c->err = "alpha must be in [0, 32]"; return MTP_EINVAL; }
+    if (c->beams && c->beams != beams) { c->err = "beams cannot change before the next prefill"; return MTP_EINVAL; }
+    for (int b = 0; b < B; ++b) {
+        const SeqState &s = c->h_state[b], &f = c->h_state[b / beams * beams];
+        if (s.phon_len != f.phon_len || s.prompt_len != f.prompt_len) {
+            c->err = "the beams of a request need prompts of one length";
+            return MTP_EINVAL;
+        }
+    }
+    int32_t* w = c->ws_ptr<int32_t>(c->ws.bm_rows);
+    BeamRowsArgs r{};
+    r.B = B; r.beams = beams; r.max_new = cf.max_new; r.maxp = (int)c->ws.maxp; r.eos_id = cf.eos_id; r.fresh = c->beams == 0;
+    r.st = c->ws_ptr<SeqState>(c->ws.state); r.hist = c->ws_ptr<int32_t>(c->ws.hist); r.btab = c->ws_ptr<int32_t>(c->ws.btab);
+    r.out_tok = c->ws_ptr<int32_t>(c->ws.out_tok); r.out_cnt = c->ws_ptr<int32_t>(c->ws.out_cnt);
+    r.score = reinterpret_cast<float*>(w); r.len = w + B; r.done = w + 2 * B; r.ctx = w + 3 * B; r.add = w + 4 * B;
+    r.parent = w + 5 * B; r.token = w + 6 * B;
+    int32_t* skip = w + 7 * B;                   // outputs of the selection and the plan that nobody reads
+    int32_t* small = w + 8 * B;
+    r.new_st = c->ws_ptr<SeqState>(c->ws.bm_state); r.new_hist = c->ws_ptr<int32_t>(c->ws.bm_hist);
+    r.new_tab = c->ws_ptr<int32_t>(c->ws.bm_tab);
+    HIPCHK(c, beam_rows_prepare(c->stream, r), "beam rows");
+    mtp_beam_args s{};
+    s.n_requests = B / beams; s.beams = beams; s.vocab = cf.vocab; s.eos_id = cf.eos_id; s.eos_min = cf.eos_min; s.alpha = alpha;
+    s.logits = c->ws_ptr<float>(c->ws.logits); s.ld = cf.vocab; s.score = r.score; s.len = r.len; s.done = r.done;
+    // (the lengths and marks before the choice are what the rows' parents have: the new ones go elsewhere)
+    s.out_score = r.score; s.out_len = skip; s.out_done = small; s.out_parent = w + 5 * B; s.out_token = w + 6 * B;
+    int rc = mtp_beam_select(&s, c->stream);
+    if (rc) { c->err = "beam selection failed"; return rc; }
+    HIPCHK(c, beam_rows_follow(c->stream, r), "beam rows");
+    mtp_plan_args p{};
+    p.n_rows = B; p.max_pages = (int32_t)c->ws.maxp; p.num_pages = (int32_t)c->ws.num_pages; p.max_tokens = 0;
+    p.parent = r.parent; p.len = r.ctx; p.add = r.add; p.table_in = r.btab; p.table = c->ws_ptr<int32_t>(c->ws.bm_tab);
+    p.row_start = small; p.kv_len = small + B + 1; p.copies = small + 2 * B + 1; p.status = small + 4 * B + 1;
+    p.workspace = c->WS() + c->ws.bm_plan; p.workspace_bytes = c->ws.bm_plan_bytes;
+    rc = mtp_pages_plan(&p, c->stream);
+    if (rc) { c->err = "beam page plan failed"; return rc; }
+    mtp_copy_args m{};
+    m.pool = c->buf.kv_pool;
+    m.page_bytes = (uint64_t)2 * cf.n_heads * cf.page_size * MTP_HEAD_DIM * c->ws.act_bytes;
+    m.n_layers = cf.n_layers; m.num_pages = (int32_t)c->ws.num_pages; m.n_copies = B; m.copies = p.copies;
+    m.layer_stride = m.page_bytes * (uint64_t)c->ws.num_pages;
+    rc = mtp_pages_copy(&m, c->stream);
+    if (rc) { c->err = "beam page copies failed"; return rc; }
+    HIPCHK(c, beam_rows_apply(c->stream, r), "beam rows");
+    c->beams = beams;
+    c->beam_ready = false;
+    if (!out_tokens && !out_parent && !out_score) return MTP_OK;
+    ToHost out{c};
+    out.add(out_tokens, r.out_tok, (size_t)B * 4, "tokens to host");
+    out.add(out_parent, r.parent, (size_t)B * 4, "parents to host");
+    out.add(out_score, r.score, (size_t)B * 4, "scores to host");
+    return out.wait();
 }
 
 int mtp_set_selection(mtp_ctx* c, int lattice, int anchored) {

@@ -15,6 +15,7 @@
 
 #include "../../include/mtp.h"
 #include "common.h"
+#include "launch.h"
 #include "wave.h"
 
 namespace mtp {
@@ -366,6 +367,50 @@ __global__ __launch_bounds__(512) void beam_merge_kernel(mtp_beam_args a, BeamWs
     beam_merge<8, false>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
 }
 
+// ------------------------------------------------- a context's beams
+__global__ __launch_bounds__(256) void beam_prepare_kernel(BeamRowsArgs a) {
+    const int b = blockIdx.x * 256 + threadIdx.x;
+    if (b >= a.B) return;
+    const int n = a.out_cnt[b];                  // a row that had ended before the step emitted nothing
+    a.len[b] = a.st[b].gen - n;
+    a.done[b] = n == 0 ? 1 : 0;
+    a.ctx[b] = a.st[b].ctx_len;
+    if (a.fresh) a.score[b] = b % a.beams == 0 ? 0.f : -INFINITY;
+}
+
+// Row c as its parent's continuation by its token.
+__global__ __launch_bounds__(256) void beam_follow_kernel(BeamRowsArgs a) {
+    const int c = blockIdx.x, p = a.parent[c], ended = a.done[p], tok = a.token[c];
+    SeqState s = a.st[p];
+    const int g = a.len[p];
+    const int32_t* from = a.hist + (size_t)p * a.max_new;
+    int32_t* to = a.new_hist + (size_t)c * a.max_new;
+    for (int i = threadIdx.x; i < g; i += 256) to[i] = from[i];
+    if (threadIdx.x != 0) return;
+    if (!ended) {
+        to[g] = tok;
+        const bool done = tok == a.eos_id || g + 1 >= a.max_new;
+        s.gen = g + 1;
+        s.done = done ? 1 : 0;
+        s.pend_len = done ? 0 : 1;
+        s.pend_ids[0] = tok;
+        s.last_tok = tok;
+    }
+    a.add[c] = s.prompt_len + a.max_new - s.ctx_len;
+    a.out_tok[c] = ended ? -1 : tok;
+    a.out_cnt[c] = ended ? 0 : 1;
+    a.new_st[c] = s;
+}
+
+__global__ __launch_bounds__(256) void beam_apply_kernel(BeamRowsArgs a) {
+    const int c = blockIdx.x;
+    const SeqState s = a.new_st[c];
+    for (int i = threadIdx.x; i < s.gen; i += 256) a.hist[(size_t)c * a.max_new + i] = a.new_hist[(size_t)c * a.max_new + i];
+    // (unused table entries name page 0, so that loads past the context stay in the pool)
+    for (int i = threadIdx.x; i < a.maxp; i += 256) a.btab[(size_t)c * a.maxp + i] = max(0, a.new_tab[(size_t)c * a.maxp + i]);
+    if (threadIdx.x == 0) a.st[c] = s;
+}
+
 bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }
 
 int beam_check(const mtp_beam_args* a) {
@@ -378,6 +423,19 @@ int beam_check(const mtp_beam_args* a) {
 }
 
 }  // namespace
+hipError_t beam_rows_prepare(hipStream_t st, const BeamRowsArgs& a) {
+    hipLaunchKernelGGL(beam_prepare_kernel, dim3((a.B + 255) / 256), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t beam_rows_follow(hipStream_t st, const BeamRowsArgs& a) {
+    hipLaunchKernelGGL(beam_follow_kernel, dim3(a.B), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t beam_rows_apply(hipStream_t st, const BeamRowsArgs& a) {
+    hipLaunchKernelGGL(beam_apply_kernel, dim3(a.B), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
 }  // namespace mtp
 
 extern "C" {

@@ -306,4 +306,20 @@ struct SelectArgs {
 // launch (one workgroup per sequence).
 hipError_t select_fused(hipStream_t st, const SelectArgs& a);
 
+// One step of beam search on a context's sequences (mtp_beam_advance): the
+// inputs of mtp_beam_select from the state that the decode step left; then,
+// its choice made, every row's new state, history and page needs, and (the
+// pages planned) the swap into place.
+struct BeamRowsArgs {
+    int B, beams, max_new, maxp, eos_id, fresh;  // fresh: the search starts, only each request's first beam counts
+    SeqState* st; int32_t* hist; int32_t* btab;
+    int32_t* out_tok; int32_t* out_cnt;          // the step's outputs
+    float* score; int32_t* len; int32_t* done; int32_t* ctx; int32_t* add;
+    const int32_t* parent; const int32_t* token;
+    SeqState* new_st; int32_t* new_hist; const int32_t* new_tab;
+};
+hipError_t beam_rows_prepare(hipStream_t st, const BeamRowsArgs& a);
+hipError_t beam_rows_follow(hipStream_t st, const BeamRowsArgs& a);
+hipError_t beam_rows_apply(hipStream_t st, const BeamRowsArgs& a);
+
 }  // namespace mtp

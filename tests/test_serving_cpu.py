@@ -249,3 +249,18 @@ def test_struct_layout_matches_the_header(tmp_path):
         assert int(got[n]) == ctypes.sizeof(s)
         for f in s._fields_:
             assert int(got[f"{n}.{f[0]}"]) == getattr(s, f[0]).offset, (n, f[0])
+
+
+def test_beam_advance_refuses_without_a_step():
+    from paper_2410_13839_amd import binding as b
+    from paper_2410_13839_amd.workloads import WORKLOADS
+    wl = WORKLOADS["valle_k4"]
+    cfg = b.make_config(wl.model, 4, wl.max_prompt, wl.max_new, wl.eos_min)
+    ctx = b.mtp_create(cfg, b.mtp_buffers(256, 512, 1024, 2048), 0)
+    try:
+        with pytest.raises(b.MTPError) as e:
+            b.mtp_beam_advance(ctx, 4, 4)
+        assert e.value.code == b.MTP_ESTATE
+    finally:
+        b.mtp_destroy(ctx)
+    assert b.mtp_query_sizes(cfg).workspace_bytes > 4 * wl.max_new * 4 * 2
