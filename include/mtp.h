@@ -502,8 +502,8 @@ typedef struct mtp_cache {
  * Two rows of table_in must not hold the same partly filled last page unless
  * they are not both continued.  table may be table_in when parent is NULL;
  * every other pair of arrays must be disjoint.  0 <= n_rows <= 4096,
- * 1 <= max_pages <= 65536, 1 <= num_pages < 2^27, 0 <= max_tokens < 2^31;
- * len[p] + add[c] <= 16 * max_pages.  Arrays are 4-byte aligned, the
+ * 1 <= max_pages <= 65536, n_rows * max_pages < 2^27, 1 <= num_pages < 2^27,
+ * 0 <= max_tokens < 2^31; len[p] + add[c] <= 16 * max_pages.  Arrays are 4-byte aligned, the
  * workspace (about num_pages / 8 + 16 n_rows bytes; none, and NULL, when the
  * size call reports 0) 256-byte. */
 typedef struct mtp_plan_args {

@@ -864,14 +864,14 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     // 256 keys (narrow: 128).  Narrow: keys below 512 stay whole (400 keys of 16 heads 7.4 us whole, 8.1 us in three
     // runs), so do tiles that fill three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us whole, 38 us
     // in three), at most 32 runs (16,000 keys of 8 KV heads 26 us, 33 us in 64); of a long cache runs of 2560 keys, which
-    // even out ragged rows (32 rows of up to 16,384 keys 257 us in two runs, 220 us in seven).
+    // even out ragged rows (32 rows of up to 16,384 keys 257 us in two runs, 220 us in six) while the tiles are few.
     int64_t n;
     if (x.wide) {
         const int64_t want = d128 ? 512 : 1024;
         n = std::min<int64_t>((want + work - 1) / work, kv / 256);
     } else {
         n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>((512 + work - 1) / work, kv / 128), 32);
-        if (kv >= 8192) n = std::max<int64_t>(n, kv / 2560);
+        if (kv >= 8192) n = std::max<int64_t>(n, std::min<int64_t>(kv / 2560, 4096 / work));
     }
     n = std::max<int64_t>(1, std::min<int64_t>(n, MAX_RUNS));
     x.g.n_splits = (int)n;

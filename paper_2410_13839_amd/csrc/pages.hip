@@ -61,20 +61,19 @@ uint64_t plan_carve(const mtp_plan_args& a, PlanWs* w) {
 
 // Exclusive sums over the workgroup's NT threads; v becomes the sum of the
 // threads before, the result is the total.  buf: NT / 64 values of LDS.
-template <int NT, typename V>
-__device__ __forceinline__ V block_scan(V& v, V* buf) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const V own = v;
-    V x = v;
+template <int NT>
+__device__ __forceinline__ int block_scan(int& v, int* buf) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, own = v;
+    int x = v;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const V y = __shfl_up(x, o);
+        const int y = __shfl_up(x, o);
         if (lane >= o) x += y;
     }
     __syncthreads();                   // (buf may still be read from the last call)
     if (lane == 63) buf[wave] = x;
     __syncthreads();
-    V before = 0, total = 0;
+    int before = 0, total = 0;
     for (int i = 0; i < NT / 64; ++i) {
         before += i < wave ? buf[i] : 0;
         total += buf[i];
@@ -86,7 +85,7 @@ __device__ __forceinline__ V block_scan(V& v, V* buf) {
 // Step 1 by one workgroup of NT threads: rows, row_start, kv_len, status.
 // low: n_rows words of LDS.
 template <int NT, int PER>
-__device__ __forceinline__ void plan_rows(const mtp_plan_args& a, PlanRow* rows, int* low, long long* buf_t, int* buf_f) {
+__device__ __forceinline__ void plan_rows(const mtp_plan_args& a, PlanRow* rows, int* low, int* buf) {
     const int tid = threadIdx.x, n = a.n_rows;
     for (int c = tid; c < n; c += NT) low[c] = 0x7fffffff;
     __syncthreads();
@@ -110,31 +109,27 @@ __device__ __forceinline__ void plan_rows(const mtp_plan_args& a, PlanRow* rows,
         bad += ok ? 0 : 1;
     }
     __syncthreads();
-    long long tokens = 0;              // of the slabs before
-    int pages = 0;
+    int tokens = 0, pages = 0;         // of the slabs before (fewer than 2^31: the table holds fewer than 2^27 pages)
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         if (NT * k >= n) break;        // uniform
         const int c = tid + NT * k;
         const bool in = c < n;
         if (in && a.parent && r[k].y % PG && low[r[k].x] != c) r[k].z |= (int)0x80000000;
-        long long t = in ? row_new(r[k]) : 0;
-        int f = in ? row_need(r[k]) - row_kept(r[k]) : 0;
-        const long long tt = block_scan<NT>(t, buf_t);
-        const int ff = block_scan<NT>(f, buf_f);
+        int t = in ? row_new(r[k]) : 0, f = in ? row_need(r[k]) - row_kept(r[k]) : 0;
+        const int tt = block_scan<NT>(t, buf), ff = block_scan<NT>(f, buf);
         if (in) {
             r[k].w = pages + f;
             rows[c] = r[k];
-            const long long s = tokens + t;
-            a.row_start[c] = (int)(s < 0x7fffffff ? s : 0x7fffffff);
+            a.row_start[c] = tokens + t;
             a.kv_len[c] = r[k].y + row_new(r[k]);
         }
         tokens += tt;
         pages += ff;
     }
-    const int all_bad = block_scan<NT>(bad, buf_f);
+    const int all_bad = block_scan<NT>(bad, buf);
     if (tid == 0) {
-        a.row_start[n] = (int)(tokens < 0x7fffffff ? tokens : 0x7fffffff);
+        a.row_start[n] = tokens;
         a.status[0] = 0;
         a.status[1] = all_bad;
         a.status[2] = 0;
@@ -249,10 +244,9 @@ __device__ __forceinline__ void plan_rest(const mtp_plan_args& a, int64_t tokens
 }
 
 __global__ __launch_bounds__(ROWS_T) void plan_rows_kernel(mtp_plan_args a, PlanWs w) {
-    __shared__ int s_low[MAX_ROWS], s_f[ROWS_T / 64];
-    __shared__ long long s_t[ROWS_T / 64];
+    __shared__ int s_low[MAX_ROWS], s_buf[ROWS_T / 64];
     if (blockIdx.x == 0) {
-        plan_rows<ROWS_T, MAX_ROWS / ROWS_T>(a, w.rows, s_low, s_t, s_f);
+        plan_rows<ROWS_T, MAX_ROWS / ROWS_T>(a, w.rows, s_low, s_buf);
         return;
     }
     const int words = (a.num_pages + 31) / 32;
@@ -278,15 +272,14 @@ __global__ __launch_bounds__(PLAN_T) void plan_assign_kernel(mtp_plan_args a, Pl
 __global__ __launch_bounds__(ROWS_T) void plan_one_kernel(mtp_plan_args a, int per) {
     __shared__ uint32_t s_bits[ONE_WORDS];
     __shared__ PlanRow s_rows[ONE_ROWS];
-    __shared__ int s_low[ONE_ROWS], s_f[ROWS_T / 64], s_before[ROWS_T + 1];
-    __shared__ long long s_t[ROWS_T / 64];
+    __shared__ int s_low[ONE_ROWS], s_buf[ROWS_T / 64], s_before[ROWS_T + 1];
     const int words = (a.num_pages + 31) / 32, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = threadIdx.x; i < words; i += ROWS_T) s_bits[i] = 0u;
-    plan_rows<ROWS_T, 1>(a, s_rows, s_low, s_t, s_f);
+    plan_rows<ROWS_T, 1>(a, s_rows, s_low, s_buf);
     __syncthreads();
     for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_mark(a, s_rows[c], s_bits, lane, 64);
     __syncthreads();
-    plan_count<ROWS_T>(s_bits, a.num_pages, per, s_before, s_f);
+    plan_count<ROWS_T>(s_bits, a.num_pages, per, s_before, s_buf);
     for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_table<ROWS_T>(a, c, s_rows[c], s_bits, per, s_before, lane, 64);
     __syncthreads();
     for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_slots(a, c, s_rows[c], a.row_start[c], lane, 64);
@@ -298,7 +291,7 @@ bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) 
 int plan_check(const mtp_plan_args* a) {
     if (!a) return MTP_EINVAL;
     if (a->n_rows < 0 || a->n_rows > MAX_ROWS || a->max_pages < 1 || a->max_pages > 65536 || a->num_pages < 1 ||
-        a->num_pages >= (1 << 27) || a->max_tokens < 0)
+        a->num_pages >= (1 << 27) || a->max_tokens < 0 || (int64_t)a->n_rows * a->max_pages >= (1 << 27))
         return MTP_EINVAL;
     return MTP_OK;
 }

@@ -122,6 +122,8 @@ def _rows(t: torch.Tensor, name: str, pool: torch.Tensor, dim: int, heads: Optio
     s0, s1, s2 = t.stride()
     if shape[0] and (s2 != 1 or (s1 != dim and shape[1] > 1)):
         raise ValueError(f"{name}: a token's heads must be contiguous")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: the serving operators have no backward pass (call them under torch.no_grad)")
     return s0 if shape[0] > 1 else shape[1] * dim
 
 
@@ -228,6 +230,7 @@ def select_beams(logits: torch.Tensor, score: torch.Tensor, length: torch.Tensor
     _need(logits.dim() == 3 and logits.dtype == torch.float32, "logits: float32 [requests, beams, vocab]")
     r, w, v = logits.shape
     ld = logits.stride(1) if w > 1 else (logits.stride(0) if r > 1 else v)
+    _need(not (logits.requires_grad and torch.is_grad_enabled()), "logits: no backward pass (call under torch.no_grad)")
     _need(v == 0 or logits.stride(2) == 1 or v == 1, "logits: a row's logits must be contiguous")
     _need(r <= 1 or w <= 1 or logits.stride(0) == w * ld, "logits: the rows must be evenly spaced")
     _need(score.dtype == torch.float32 and tuple(score.shape) == (r, w) and score.device == dev and score.is_contiguous(),

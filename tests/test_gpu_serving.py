@@ -319,6 +319,44 @@ def test_attention_key_hint_changes_no_result_beyond_rounding(max_kv):
         check_attention(attention_case(13, [3000, 17, 900], [q, 1, q], 4, 2, 64, torch.bfloat16), max_kv=max_kv)
 
 
+@pytest.mark.parametrize("n,kv_hi,q_hi,HQ,H,D", [(4096, 20, 1, 1, 1, 64), (300, 40, 3, 2, 1, 128), (100, 60, 40, 4, 2, 64),
+                                                (65, 70, 30, 4, 1, 128), (64, 70, 1, 2, 2, 128)])
+def test_attention_many_rows(n, kv_hi, q_hi, HQ, H, D):
+    rng = np.random.default_rng(n)
+    q = rng.integers(0, q_hi + 1, n)
+    q[0] = q_hi
+    check_attention(attention_case(n, rng.integers(0, kv_hi + 1, n), q, HQ, H, D, torch.bfloat16), causal=q_hi > 1)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attention_starts_and_lengths_outside_their_range_are_clamped(dtype):
+    c = attention_case(2, [40, 30, 50], [3, 4, 70], 4, 2, 64, dtype, nan_behind=False)
+    c["row_start"] = np.array([-9, 3, 7, 2 ** 31 - 1], np.int32)
+    c["kv_len"] = np.array([2 ** 31 - 1, -2 ** 31, 50], np.int32)
+    c["T"] = 77
+    c["table"] = np.where(c["table"] < 0, 1, c["table"]).astype(np.int32)
+    q = c["q"][:77]
+    want = np.zeros((77, 4, 64))
+    bound = np.zeros((2, 77, 4, 64))
+    bf = dtype == torch.bfloat16
+    paging.attend(c["pool"].float().numpy(), bf, c["table"], c["row_start"], c["kv_len"], q.float().numpy().reshape(77, 4, 64),
+                  want, bound=bound)
+    got = host(serving().attend_pages(c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"]),
+                                      q.cuda().view(77, 4, 64)).float())
+    tol = bound[0] * (2.0 ** -8 if bf else 0.0) + np.abs(want) * (2.0 ** -8 if bf else 0.0) + 1e-4 * bound[0] + 1e-30
+    assert (np.abs(got - want) <= tol).all()
+
+
+def test_calls_that_need_a_gradient_are_refused():
+    c = attention_case(2, [40], [3], 4, 2, 64, torch.float32)
+    q = c["q"][:3].cuda().view(3, 4, 64).requires_grad_()
+    args = (c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"]), q)
+    with pytest.raises(ValueError):
+        serving().attend_pages(*args)
+    with torch.no_grad():
+        serving().attend_pages(*args)
+
+
 def test_attention_is_reproducible():
     c = attention_case(17, [4000, 900, 2000], [1, 1, 1], 8, 2, 128, torch.bfloat16)
     a = run_attention(c)

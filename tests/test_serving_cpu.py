@@ -56,7 +56,8 @@ def _refused(call, args, code=None):
 
 
 @pytest.mark.parametrize("kw", [dict(n_rows=-1), dict(n_rows=4097), dict(max_pages=0), dict(max_pages=65537),
-                                dict(num_pages=0), dict(num_pages=1 << 27), dict(max_tokens=-1), dict(len=0), dict(add=0),
+                                dict(n_rows=4096, max_pages=32768), dict(num_pages=0), dict(num_pages=1 << 27),
+                                dict(max_tokens=-1), dict(len=0), dict(add=0),
                                 dict(table_in=0), dict(table=0), dict(row_start=0), dict(kv_len=0), dict(slots=0),
                                 dict(positions=0), dict(copies=0), dict(status=0), dict(workspace=0),
                                 dict(workspace=4096 + 128), dict(len=258), dict(parent=254), dict(parent=256, table=768)])
