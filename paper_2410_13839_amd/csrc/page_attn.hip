@@ -126,10 +126,10 @@ __device__ __forceinline__ uint32_t inside2(int y, int lo, int hi) {
 
 // ------------------------------------------------------------ few query rows
 //
-// One workgroup per (tile of 16 query rows, KV head block, run of keys); its NW
-// waves take 32 keys (two pages) in turn, each with its own running maximum,
-// sum and output, merged through LDS once at the end.  Keys and values go
-// straight from the cache into the operands of the matrix products, the next
+// One workgroup per (tile of 16 query rows, KV head block, run of keys); its
+// four waves take 32 keys (two pages) in turn, each with its own running
+// maximum, sum and output, merged through LDS once at the end.  Keys and values
+// go straight from the cache into the operands of the matrix products, the next
 // 32 keys' loads in flight while the current ones are used:
 //   S^T[key][q] = K[key][:] . Q[q][:]
 //   O^T[dim][q] += V^T[dim][key] P^T[key][q]
@@ -139,6 +139,13 @@ __device__ __forceinline__ uint32_t inside2(int y, int lo, int hi) {
 // transposed V block.  fp32 (16 keys a product): the contraction's index g of
 // step e is dimension 16 j + 4 g + e, or key 4 g + e, and row r of the output
 // tile dt is dimension (D / 16) r + dt, all 16-byte loads again.
+//
+// What bounds it: HBM where there are many keys (32 single tokens over 512 to
+// 16,384 keys, 1.1 GB: 220 us, 5.0 TB/s, what a large copy reaches), the chain
+// of loads lengths -> table -> keys and the second launch where there are few (4
+// tokens over 1075 keys of 16 heads 9.0 us; with 16 waves a head in one launch
+// 11.8 us: a CU alone draws 25 to 50 GB/s).  A lookup of all rows' lengths in one
+// round of loads cost registers and measured slower.
 constexpr int NW = 4;
 
 template <typename T, int D>
@@ -444,12 +451,28 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
 // Row 16 s + 8 j + 4 h + e of a 32-key tile of S is key 16 s + 8 h + 4 j + e, so
 // that lane (q, h) holds the keys 16 s + 8 h .. + 7 in its registers 8 s .. 8 s
 // + 7: its operand of the second product, the other one being 16 bytes of a V
-// page.  In LDS a page's V block is as in the cache (a wave's operand reads are
-// 1 KB in a row); K rows are whole multiples of the banks, so the 16-byte
-// pieces of a row are stored in an order that its slot shifts (the address that
-// a lane loads from, not where it stores).
+// page.  K rows and V pages are whole multiples of the banks, so their 16-byte
+// pieces are stored in an order that slot and dimension shift (the address that
+// a lane loads from, not where it stores): 16 lanes then read 16 different
+// banks' pieces.
 // The reference m moves only when a score exceeds it by 8 (float32 sums and
-// bf16 probabilities up to 2^8 keep their relative precision).
+// bf16 probabilities up to 2^8 keep their relative precision).  Probabilities
+// are rounded to bf16, as the matrix product takes them; their sum is not.
+// Blocks that every query of the tile sees whole run in a loop of their own,
+// without masks: in one loop with the others the accumulators were copied every
+// block (367 us instead of 320 us below).
+//
+// What bounds it: the matrix cores and the vector unit in turn.  A block costs a
+// wave 1000 cycles of products and as many of exponentials, maxima, sums and
+// conversions; counters show each busy 42 to 44% of the time, the two waves of a
+// SIMD overlapping little.  Forming the next block's scores during the
+// exponentials (software pipelining) measured the same and cost registers; so
+// did a third block in LDS, raised priority around the products, and tiles
+// dealt longest first.  Measured, 32 query heads on 8 KV heads of 128: chunks of
+// 512 tokens over 8192 keys 314 us (848 TFLOP/s), whole prompts of 4096 623 us
+// (880), chunks of up to 512 over 2048 to 8192 keys 213 us (685: the longest
+// rows' workgroups finish last); 16 heads of 64, 450-token prompts 23.3 us.
+// Head dim 64 with four workgroups a CU instead of three: 230 -> 199 us.
 constexpr int TR = 128;                          // query rows of a tile
 constexpr int KB = 64;                           // keys of a block
 
@@ -457,7 +480,7 @@ typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
 template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_tile_kernel(mtp_attention_args a, AttnGeo g) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_attention_args a, AttnGeo g) {
     constexpr float MSTEP = 8.0f;
     constexpr int CW = D / 8;                    // 16-byte pieces of a K row
     __shared__ __attribute__((aligned(1024))) bf16_t s_k[2][KB * D], s_v[2][KB * D];
@@ -813,7 +836,7 @@ __global__ __launch_bounds__(64 * JW) void attn_join_kernel(mtp_attention_args a
 }
 
 // ------------------------------------------------------------------- launches
-// (Four rows a wave where there are few runs: two runs of 488 wide tiles 28 us with one row a wave, JOIN4; many
+// (Four rows a wave where there are few runs: two runs of 488 wide tiles 28 us with one row a wave, 15 us; many
 // runs of few tiles are faster with a row each: 11 runs of 48 wide tiles, the whole call 51.5 and 41 us.)
 template <typename T, int D, int RT>
 void join_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g, unsigned work) {
@@ -860,19 +883,17 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     x.g.tt = rt / x.g.gs;
     x.g.n_tiles = a.n_tokens / x.g.tt + a.n_rows;
     const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
-    // Runs of the keys: as many workgroups as the CUs hold at once (wide, head dim 64: three a CU), no run shorter than
-    // 256 keys (narrow: 128).  Narrow: keys below 512 stay whole (400 keys of 16 heads 7.4 us whole, 8.1 us in three
-    // runs), so do tiles that fill three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us whole, 38 us
-    // in three), at most 32 runs (16,000 keys of 8 KV heads 26 us, 33 us in 64); of a long cache runs of 2560 keys, which
-    // even out ragged rows (32 rows of up to 16,384 keys 257 us in two runs, 220 us in six) while the tiles are few.
+    // Runs of the keys: as many workgroups as the CUs hold at once (wide: two a CU with head dim 128, three with 64; four
+    // fit, but 128 tokens over 8000 keys take 31 us then, 28.5 us with three), no run shorter than 256 keys (narrow:
+    // 128).  Narrow: keys below 512 stay whole (400 keys of 16 heads 7.4 us whole, 8.1 us in three runs), so do tiles that
+    // fill three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us whole, 38 us in three), at most 32
+    // runs (16,000 keys of 8 KV heads 26 us, 33 us in 64).  Of a long cache runs of 2560 keys, which even out ragged
+    // rows, while the tiles are few (32 rows of up to 16,384 keys: 4 query rows each 257 us in two runs, 220 us in six; 8
+    // each, wide, 269 and 212 us).
     int64_t n;
-    if (x.wide) {
-        const int64_t want = d128 ? 512 : 1024;
-        n = std::min<int64_t>((want + work - 1) / work, kv / 256);
-    } else {
-        n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>((512 + work - 1) / work, kv / 128), 32);
-        if (kv >= 8192) n = std::max<int64_t>(n, std::min<int64_t>(kv / 2560, 4096 / work));
-    }
+    if (x.wide) n = std::min<int64_t>(((d128 ? 512 : 768) + work - 1) / work, kv / 256);
+    else n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>((512 + work - 1) / work, kv / 128), 32);
+    if (kv >= 8192) n = std::max<int64_t>(n, std::min<int64_t>(kv / 2560, 4096 / work));
     n = std::max<int64_t>(1, std::min<int64_t>(n, MAX_RUNS));
     x.g.n_splits = (int)n;
     x.g.split_len = (int)(((kv + n - 1) / n + KB - 1) / KB * KB);
