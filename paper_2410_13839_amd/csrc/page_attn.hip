@@ -888,12 +888,13 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     // 128).  Narrow: keys below 512 stay whole (400 keys of 16 heads 7.4 us whole, 8.1 us in three runs), so do tiles that
     // fill three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us whole, 38 us in three), at most 32
     // runs (16,000 keys of 8 KV heads 26 us, 33 us in 64).  Of a long cache runs of 2560 keys, which even out ragged
-    // rows, while the tiles are few (32 rows of up to 16,384 keys: 4 query rows each 257 us in two runs, 220 us in six; 8
-    // each, wide, 269 and 212 us).
+    // rows, while the tiles are few and part full (32 rows of up to 16,384 keys: 4 query rows each 257 us in two runs, 220
+    // us in six; 8 each, wide, 269 and 212 us; full tiles, 512 of them over 8192 keys: 314 us whole, 365 us in three).
+    const bool few = (int64_t)a.n_tokens * x.g.gs <= (int64_t)TR * a.n_rows;
     int64_t n;
     if (x.wide) n = std::min<int64_t>(((d128 ? 512 : 768) + work - 1) / work, kv / 256);
     else n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>((512 + work - 1) / work, kv / 128), 32);
-    if (kv >= 8192) n = std::max<int64_t>(n, std::min<int64_t>(kv / 2560, 4096 / work));
+    if (kv >= 8192 && few) n = std::max<int64_t>(n, std::min<int64_t>(kv / 2560, 4096 / work));
     n = std::max<int64_t>(1, std::min<int64_t>(n, MAX_RUNS));
     x.g.n_splits = (int)n;
     x.g.split_len = (int)(((kv + n - 1) / n + KB - 1) / KB * KB);
