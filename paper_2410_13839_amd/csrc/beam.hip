@@ -211,12 +211,14 @@ struct BeamLds {
     int place[MAX_BEAMS * MAX_BEAMS];            // each candidate's place among all
 };
 
-// The request's state (the caller synchronises).
+// The request's state, by the workgroup's last wave (read after a barrier).
+template <int NW>
 __device__ __forceinline__ void beam_state(const mtp_beam_args& a, int r, BeamLds& s) {
-    if ((int)threadIdx.x >= a.beams) return;
-    const int row = r * a.beams + threadIdx.x, dn = a.done[row] > 0, len = a.len[row] + (dn ? 0 : 1);
-    s.done[threadIdx.x] = dn; s.len[threadIdx.x] = len; s.score[threadIdx.x] = a.score[row];
-    s.den[threadIdx.x] = a.alpha == 0.f ? 1.0 : pow((double)max(len, 1), (double)a.alpha);
+    const int b = (int)threadIdx.x - 64 * (NW - 1);
+    if (b < 0 || b >= a.beams) return;
+    const int row = r * a.beams + b, dn = a.done[row] > 0, len = a.len[row] + (dn ? 0 : 1);
+    s.done[b] = dn; s.len[b] = len; s.score[b] = a.score[row];
+    s.den[b] = a.alpha == 0.f ? 1.0 : pow((double)max(len, 1), (double)a.alpha);
 }
 
 // A request's merge by a workgroup of NW waves.  max, sum, list: the request's
@@ -227,7 +229,7 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
                                            const float2* list, int chunks, BeamLds& s) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.beams, n = min(W, a.vocab);
     for (int b = wave; b < W; b += NW) {
-        if (s.done[b]) continue;                 // uniform over the wave
+        if (a.done[r * W + b] > 0) continue;     // uniform over the wave
         const float2* bl = list + (size_t)b * chunks * W;
         const int entries = chunks * W;
         BeamList<4> few;                         // (its loads in flight during the sums below)
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(64 * NW) void beam_fused_kernel(mtp_beam_args a) {
     __shared__ double s_sum[FUSED_UNITS];
     const int r = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = a.beams;
     const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
-    beam_state(a, r, s);
+    beam_state<NW>(a, r, s);
     for (int u = wave; u < W * chunks; u += NW) {
         const int b = u / chunks;
         if (a.done[r * W + b] > 0) continue;
@@ -359,12 +361,12 @@ __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs
     beam_chunk(a, row, ch, w.list + u * a.beams, &w.max[u], &w.sum[u], s_buf[wave]);
 }
 
-__global__ __launch_bounds__(512) void beam_merge_kernel(mtp_beam_args a, BeamWs w, int chunks) {
+template <int NW, bool FEW>
+__global__ __launch_bounds__(64 * NW) void beam_merge_kernel(mtp_beam_args a, BeamWs w, int chunks) {
     __shared__ BeamLds s;
     const size_t u = (size_t)blockIdx.x * a.beams * chunks;
-    beam_state(a, blockIdx.x, s);
-    __syncthreads();
-    beam_merge<8, false>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
+    beam_state<NW>(a, blockIdx.x, s);
+    beam_merge<NW, FEW>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
 }
 
 // ------------------------------------------------- a context's beams
@@ -468,7 +470,10 @@ int mtp_beam_select(const mtp_beam_args* args, void* hip_stream) {
         else hipLaunchKernelGGL(beam_fused_kernel<16>, dim3(a.n_requests), dim3(1024), 0, st, a);
     } else {
         hipLaunchKernelGGL(beam_chunk_kernel, dim3((chunks + 3) / 4, a.n_requests * a.beams), dim3(256), 0, st, a, w, chunks);
-        hipLaunchKernelGGL(beam_merge_kernel, dim3(a.n_requests), dim3(512), 0, st, a, w, chunks);
+        if (a.beams * chunks <= 256)
+            hipLaunchKernelGGL((beam_merge_kernel<16, true>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
+        else
+            hipLaunchKernelGGL((beam_merge_kernel<8, false>), dim3(a.n_requests), dim3(512), 0, st, a, w, chunks);
     }
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
