@@ -9,7 +9,15 @@
 // group maxima bounds the last of them from below, what reaches the bound is
 // gathered into LDS (a few dozen logits) and taken best first.  A request's
 // workgroup then merges the sorted lists of each beam's chunks, and the beams'
-// lists in float64.  With few chunks all of it is one launch.
+// lists in float64, where a candidate's place is the number of others before it
+// (a binary search in every other beam's list).  With few chunks all of it is
+// one launch.
+// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 12 us
+// for the chunks (2.8 TB/s; 4096 waves load at once and then compute: the
+// exponentials, and eight rounds of places) and 8 us for the merge, a chain of
+// loads, a float64 exponential, logarithm and power, and eight rounds of a wave
+// maximum per beam.  One request of 4 beams over 1025 logits 8 us: the launch and
+// the same chain.
 #include <hip/hip_runtime.h>
 #include <math.h>
 

@@ -7,6 +7,9 @@
 // marks the pages that it keeps in a bitmap; every row takes its fresh pages by
 // rank among the clear bits and writes its table row, slots and positions.
 // Small plans run the three steps in one workgroup with the bitmap in LDS.
+// What bounds it: the chain of dependent loads (parent -> lengths -> table ->
+// bitmap) and the launches, not bytes: 256 rows of 250 pages, 0.5 MB, 14.7 us in
+// three launches; 8 rows of 229 pages 7.9 us in one.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -306,6 +309,10 @@ int plan_check(const mtp_plan_args* a) {
 // octet belongs to its first token's group, which also loads the up to seven
 // tokens behind its own; every group looks at 7 + 48 + 7 slots, a lane each, so
 // that all agree on the octets wherever the groups' borders fall.
+// What bounds it: HBM.  32 prompts of 200 to 450 tokens, 16 heads of 64 in bf16
+// (85 MB read and written): 18 us warm, 25 us from HBM (3.4 TB/s; groups of 16
+// tokens without the look around, 31 us: octets across their borders were
+// stored in two-byte pieces), fp32 37 us (4.6 TB/s).
 constexpr int WOWN = 48, WEXT = 7;     // a group's own tokens, tokens looked at on either side
 
 template <typename T, int D>
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(256) void pages_write_kernel(mtp_write_args a) {
     constexpr int STR = D + 8;                                  // padded LDS row
     constexpr bool TURN = sizeof(T) == 2;
     __shared__ __attribute__((aligned(16))) T s_v[TURN ? (WOWN + WEXT) * STR : 1];
-    __shared__ int s_slot[64];
+    __shared__ int s_slot[64], s_oct[WOWN / 8];
     const int H = a.cache.n_kv_heads, h = blockIdx.x % H, t0 = blockIdx.x / H * WOWN, tid = threadIdx.x, lane = tid & 63;
     const int lim = a.cache.num_pages * PG;
     // lane i: token t0 - 7 + i (every wave looks for itself)
@@ -322,15 +329,18 @@ __global__ __launch_bounds__(256) void pages_write_kernel(mtp_write_args a) {
     int slot = lane < WOWN + 2 * WEXT && tl >= 0 && tl < a.n_tokens ? a.slots[tl] : -1;
     if (slot < 0 || slot >= lim) slot = -1;
     if (tid < 64) s_slot[tid] = slot;
-    uint64_t heads = 0, covered = 0;                            // bit i: lane i's token
+    uint64_t heads = 0, alone = 0;     // bit i, lane i's token: the first of an octet; in none
     if constexpr (TURN) {
         const int next = __shfl_down(slot, 1);
         const uint64_t follows = __ballot(lane < 63 && slot >= 0 && next == slot + 1);
         heads = __ballot(slot >= 0 && slot % 8 == 0 && lane <= 63 - 8 && ((follows >> lane) & 0x7f) == 0x7f);
-        covered = heads | heads << 1;
+        uint64_t covered = heads | heads << 1;
         covered |= covered << 2;
         covered |= covered << 4;
-        heads &= ((1ull << WOWN) - 1) << WEXT;
+        constexpr uint64_t OWN = ((1ull << WOWN) - 1) << WEXT;
+        alone = __ballot(slot >= 0) & ~covered & OWN;
+        heads &= OWN;
+        if (tid < 64 && (heads >> lane & 1)) s_oct[__popcll(heads & ((1ull << lane) - 1))] = lane;
     }
     __syncthreads();
     T* pool = (T*)a.cache.pool;
@@ -349,27 +359,24 @@ __global__ __launch_bounds__(256) void pages_write_kernel(mtp_write_args a) {
     }
     if constexpr (TURN) {
         __syncthreads();
-        // octets two at a time: those of one page make 32 bytes in a row per dimension
-        while (heads) {
-            const int i0 = __ffsll((unsigned long long)heads) - 1;
-            heads &= heads - 1;
-            const int i1 = heads ? __ffsll((unsigned long long)heads) - 1 : -1;
-            heads &= heads - 1;                                 // (0 stays 0)
-            const int at = tid & 1 ? i1 : i0;
-            if (at < 0) continue;
-            const int s = s_slot[at];
-            T* vp = pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG;
-            const T* row = &s_v[(at - WEXT) * STR];
-            for (int d = tid >> 1; d < D; d += 128) {
-                uint32_t w[4];
+        // octets in pairs, whose 16-byte pieces alternate: those of one page make 32 bytes in a row per dimension
+        const int n = __popcll(heads);
+        for (int i = tid; i < (n + 1) / 2 * 2 * D; i += 256) {
+            const int o = i / (2 * D) * 2 + (i & 1), d = (i % (2 * D)) >> 1;
+            if (o >= n) continue;
+            const int at = s_oct[o], s = s_slot[at];
+            const T* row = &s_v[(at - WEXT) * STR + d];
+            uint32_t w[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = (uint32_t)row[2 * j * STR + d] | (uint32_t)row[(2 * j + 1) * STR + d] << 16;
-                *reinterpret_cast<uint4*>(vp + d * PG) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            for (int j = 0; j < 4; ++j) w[j] = (uint32_t)row[2 * j * STR] | (uint32_t)row[(2 * j + 1) * STR] << 16;
+            *reinterpret_cast<uint4*>(pool + (size_t)(s / PG) * 2 * H * blk + (H + h) * blk + s % PG + d * PG) =
+                make_uint4(w[0], w[1], w[2], w[3]);
         }
+        if (alone == 0) return;                                 // uniform
         for (int i = tid; i < WOWN * D; i += 256) {
-            const int tok = i / D, d = i % D, s = s_slot[WEXT + tok];
-            if (s < 0 || (covered >> (WEXT + tok) & 1)) continue;
+            const int tok = i / D, d = i % D;
+            if (!(alone >> (WEXT + tok) & 1)) continue;
+            const int s = s_slot[WEXT + tok];
             pool[(size_t)(s / PG) * 2 * H * blk + (H + h) * blk + d * PG + s % PG] = s_v[tok * STR + d];
         }
     }
@@ -382,6 +389,11 @@ void write_go(hipStream_t st, const mtp_write_args& a) {
 }
 
 // ------------------------------------------------------------------ copies
+//
+// One workgroup per (copy, layer), 16 bytes a thread and step.  Bound by HBM:
+// 0.6 x 256 pages of 64 KB in 12 layers (242 MB read and written) 46 us warm,
+// 57 us from HBM (4.2 TB/s; eight loads of a thread in flight instead of one
+// measured slower, 79 us).
 __global__ __launch_bounds__(256) void pages_copy_kernel(mtp_copy_args a) {
     const int i = blockIdx.x;
     const int src = a.copies[2 * i], dst = a.copies[2 * i + 1];
