@@ -423,7 +423,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
             const float f = s_m[w][qr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][qr] - mm);
             ll += f * s_l[w][qr];
             const f32x4_t ow = *reinterpret_cast<const f32x4_t*>(&s_acc[(w * QR + qr) * D + d]);
-            if (s_m[w][qr] != -INFINITY) v += ow * f;
+            v += ow * f;
         }
         if (live > 1) {
             *reinterpret_cast<f32x4_t*>(&g.acc[(slot + qr) * D + d]) = v;
@@ -814,7 +814,7 @@ __global__ __launch_bounds__(64 * JW) void attn_join_kernel(mtp_attention_args a
             const float w = s_w[wave][k][s];
             const f32x4_t o =
                 *reinterpret_cast<const f32x4_t*>(&g.acc[(slot + (q0 + k < rows ? k : 0) + (size_t)s * RT) * D + d]);
-            if (w != 0.f) v[k] += o * w;
+            v[k] += o * w;                       // (0 x infinity: an infinite value that is seen shows)
         }
     }
 #pragma unroll

@@ -300,6 +300,29 @@ def test_attention_what_is_not_seen_never_matters(HQ, H, D, q, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,q,max_kv", [(60, 1, 0), (200, 1, 0), (3000, 1, 0), (3000, 1, 600), (900, 130, 0), (3000, 130, 0)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_infinite_values_of_no_weight_show(D, kv, q, max_kv, dtype):
+    """Key 0 scores 65536 / sqrt(D) above every other, whose weights are then exactly 0 in float32; an infinite value of one of them, in any wave's or run's share, is not lost."""
+    c = attention_case(3, [kv], [q], 2, 1, D, dtype, nan_behind=False)
+    P, bf = c["pool"].shape[0], dtype == torch.bfloat16
+    kp = c["pool"][:, 0].view(P, 1, 16, D)
+    vp = c["pool"][:, 1].view(P, 1, D, 16) if bf else c["pool"][:, 1].view(P, 1, 16, D).transpose(2, 3)
+    kp.zero_()
+    kp[c["table"][0, 0], :, 0, 0] = 1024
+    c["q"].zero_()
+    c["q"][:, ::D] = 64                                    # scores 65536 / sqrt(D) and 0
+    for n, d in ((1, 3), (kv // 3, 17), (kv // 2, 40), (kv - q - 1 if q > 1 else kv - 1, 63)):
+        vp[c["table"][0, n // 16], :, d, n % 16] = INF
+        out = run_attention(c, max_kv=max_kv)[:q, :2 * D].reshape(q, 2, D)
+        assert not np.isfinite(out[-1, :, d]).any(), (n, d)
+    keep = [d for d in range(D) if d not in (3, 17, 40, 63)]
+    first = c["pool"][c["table"][0, 0], 1].view(D, 16)[:, 0] if bf else c["pool"][c["table"][0, 0], 1].view(16, D)[0]
+    want = np.broadcast_to(first.float().numpy()[keep], (2, len(keep)))
+    assert np.array_equal(out[-1][:, keep], want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_attention_scales(scale, dtype):
     check_attention(attention_case(5, [70, 300], [3, 80], 4, 2, 64, dtype), scale=scale)
