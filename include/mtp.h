@@ -528,9 +528,9 @@ int mtp_pages_plan(const mtp_plan_args* args, void* hip_stream);
 /* Writes the keys and values of n_tokens tokens into the cache: token t's
  * head h, k[t * k_stride + h * head_dim ..] and v likewise, in the cache's
  * type, at slots[t]; a slot outside [0, 16 * num_pages) is skipped.  Slots
- * must differ (of two equal ones either token may stay).  Strides are in
- * elements, at least n_kv_heads * head_dim; k, v and the strides' bytes are
- * multiples of 16. */
+ * must differ (two equal ones are left with a mixture of their tokens).
+ * Strides are in elements, at least n_kv_heads * head_dim; k, v and the
+ * strides' bytes are multiples of 16; ceil(n_tokens / 48) * n_kv_heads < 2^24. */
 typedef struct mtp_write_args {
     mtp_cache cache;
     int32_t n_tokens;
@@ -578,7 +578,7 @@ int mtp_pages_copy(const mtp_copy_args* args, void* hip_stream);
  * cache the probabilities are rounded to bf16 for the product with V.
  * 0 <= n_rows <= 4096, 1 <= max_pages <= 65536, 0 <= n_tokens < 2^24,
  * n_heads a multiple of n_kv_heads up to 1024, (n_tokens + n_rows) * n_heads <
- * 2^31, window >= 0 (0 with MTP_ATTN_FULL), scale finite.
+ * 2^27, window >= 0 (0 with MTP_ATTN_FULL), scale finite.
  * q, out and the bytes of their strides are multiples of 16, the strides at
  * least n_heads * head_dim; out must not overlap another operand.  The
  * workspace is 256-byte aligned (NULL when the size call reports 0). */

@@ -914,7 +914,9 @@ int attn_check(const mtp_attention_args* a) {
     if (a->n_rows < 0 || a->n_rows > 4096 || a->max_pages < 1 || a->max_pages > 65536 || a->n_tokens < 0 ||
         a->n_tokens >= (1 << 24) || a->n_heads < 1 || a->n_heads > 1024 || a->n_heads % a->cache.n_kv_heads)
         return MTP_EINVAL;
-    if ((int64_t)(a->n_tokens + a->n_rows) * a->n_heads >= (1ll << 31)) return MTP_EINVAL;
+    // (a launch holds fewer than 2^32 threads, so fewer than 2^24 workgroups: two tiles of 16 hold at least 17 query
+    // rows, the last tiles of the cache rows, part full, come to at most 4096 x 1024)
+    if ((int64_t)(a->n_tokens + a->n_rows) * a->n_heads >= (1ll << 27)) return MTP_EINVAL;
     if (a->mode != MTP_ATTN_CAUSAL && a->mode != MTP_ATTN_FULL) return MTP_EINVAL;
     if (a->window < 0 || (a->mode == MTP_ATTN_FULL && a->window != 0) || a->max_kv < 0 || !isfinite(a->scale * LOG2E))
         return MTP_EINVAL;

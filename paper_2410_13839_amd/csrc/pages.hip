@@ -472,7 +472,8 @@ int mtp_pages_write(const mtp_write_args* args, void* hip_stream) {
         a.k_stride % per || a.v_stride % per)
         return MTP_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (((int64_t)a.n_tokens + WOWN - 1) / WOWN * a.cache.n_kv_heads >= (1ll << 31)) return MTP_EINVAL;
+    // (a launch holds fewer than 2^32 threads)
+    if (((int64_t)a.n_tokens + WOWN - 1) / WOWN * a.cache.n_kv_heads >= (1ll << 24)) return MTP_EINVAL;
     if (a.cache.dtype == MTP_DTYPE_BF16) a.cache.head_dim == 64 ? write_go<bf16_t, 64>(st, a) : write_go<bf16_t, 128>(st, a);
     else a.cache.head_dim == 64 ? write_go<float, 64>(st, a) : write_go<float, 128>(st, a);
     return launched();

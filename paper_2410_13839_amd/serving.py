@@ -107,6 +107,8 @@ def _cache(pool: torch.Tensor) -> _b.mtp_cache:
     if pool.dim() != 4 or pool.dtype not in _DTYPE or not pool.is_contiguous():
         raise ValueError("pool: a contiguous float32 or bfloat16 tensor [pages, 2, kv heads, 16 * head dim]")
     pages, two, heads, block = pool.shape
+    if pool.requires_grad and torch.is_grad_enabled():
+        raise ValueError("pool: the serving operators have no backward pass (call them under torch.no_grad)")
     if two != 2 or block not in (PAGE * 64, PAGE * 128):
         raise ValueError(f"pool: [pages, 2, kv heads, 16 * 64 or 16 * 128], not {tuple(pool.shape)}")
     return _b.mtp_cache(pool.data_ptr(), _DTYPE[pool.dtype], pages, heads, block // PAGE)
@@ -186,8 +188,8 @@ def copy_pages(pools: torch.Tensor, copies: torch.Tensor) -> None:
     page_bytes = pools.shape[-3] * pools.shape[-2] * pools.shape[-1] * pools.element_size()
     _need(copies.dim() == 2, "copies: [n, 2]")
     p = _ints(copies, "copies", (copies.shape[0], 2), dev)
-    _launch(_b.mtp_pages_copy, _b.mtp_copy_args(pools.data_ptr(), page_bytes, pages * page_bytes, layers, pages,
-                                                copies.shape[0], p), dev)
+    _launch(_b.mtp_pages_copy, _b.mtp_copy_args(pools.data_ptr(), page_bytes, pages * page_bytes, _i32(layers, "layers"), pages,
+                                                _i32(copies.shape[0], "copies"), p), dev)
 
 
 def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor,
@@ -197,7 +199,8 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
     (mtp_pages_attention): causal chunks (the queries are their rows' last
     positions, `window` > 0 of them visible), or full attention with causal =
     False.  scale defaults to head dim ** -0.5.  Tokens outside every row keep
-    what `out` holds (a new `out` starts undefined there)."""
+    what `out` holds (a new `out` starts undefined there); out shares no element
+    with q or the pool."""
     dev = _device(pool, "pool")
     cache = _cache(pool)
     dim = cache.head_dim
@@ -237,7 +240,8 @@ def select_beams(logits: torch.Tensor, score: torch.Tensor, length: torch.Tensor
           "score: contiguous float32 [requests, beams] on the logits' device")
     new = torch.empty((5, r, w), dtype=torch.int32, device=dev)
     base, step = new.data_ptr(), 4 * r * w
-    args = _b.mtp_beam_args(_i32(r, "requests"), w, _i32(v, "vocab"), _i32(eos_id, "eos_id"), _i32(eos_min, "eos_min"), alpha, logits.data_ptr(), ld, score.data_ptr(),
+    args = _b.mtp_beam_args(_i32(r, "requests"), _i32(w, "beams"), _i32(v, "vocab"), _i32(eos_id, "eos_id"),
+                            _i32(eos_min, "eos_min"), alpha, logits.data_ptr(), ld, score.data_ptr(),
                             _ints(length, "length", (r, w), dev), _ints(done, "done", (r, w), dev), base, base + step,
                             base + 2 * step, base + 3 * step, base + 4 * step, None, 0)
     ws = _workspace(_b.mtp_beam_select_workspace_size, args, dev)

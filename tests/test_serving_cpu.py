@@ -265,3 +265,23 @@ def test_beam_advance_refuses_without_a_step():
     finally:
         b.mtp_destroy(ctx)
     assert b.mtp_query_sizes(cfg).workspace_bytes > 4 * wl.max_new * 4 * 2
+
+
+def test_calls_of_more_threads_than_a_launch_holds_are_refused():
+    from paper_2410_13839_amd import binding as b
+    wide = dict(n_kv_heads=1024, dtype=b.MTP_DTYPE_F32)
+    a = _attention(_cache(**wide), n_heads=1024, n_tokens=1 << 18, q_stride=1 << 16, out_stride=1 << 16)
+    _refused(b.mtp_pages_attention, a)                   # 2^24 tiles of 16 rows
+    with pytest.raises(b.MTPError):
+        b.mtp_pages_attention_workspace_size(a)
+    _refused(b.mtp_pages_write, b.mtp_write_args(_cache(**wide), 48 << 14, 256, 512, 1024, 1 << 16, 1 << 16))
+
+
+def test_a_pool_that_needs_a_gradient_is_refused():
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_amd import serving
+    pool = torch.zeros(4, 2, 1, 1024, requires_grad=True)
+    with pytest.raises(ValueError):
+        serving._cache(pool)
+    with torch.no_grad():
+        assert serving._cache(pool).num_pages == 4
