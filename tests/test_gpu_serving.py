@@ -634,3 +634,108 @@ def test_calls_on_another_stream():
     torch.cuda.synchronize()
     for o in outs:
         assert np.array_equal(o, want)
+
+
+def test_beam_select_in_place():
+    """The out arrays may be the in arrays, with one launch and with two."""
+    from paper_2410_13839_amd import binding as b
+    rng = np.random.default_rng(8)
+    for R, W, V in ((3, 4, 700), (2, 8, 20000)):
+        lg, score = rng.standard_normal((R, W, V)).astype(np.float32), -rng.random((R, W)).astype(np.float32)
+        ln, dn = rng.integers(1, 9, (R, W)), rng.integers(0, 2, (R, W))
+        want = serving().select_beams(dev(lg, torch.float32), dev(score, torch.float32), dev(ln), dev(dn), 5, 3, 0.6)
+        x = dict(score=dev(score, torch.float32), length=dev(ln), done=dev(dn), parent=dev(dn * 0), token=dev(dn * 0))
+        x_lg = dev(lg, torch.float32)
+        p = {k: t.data_ptr() for k, t in x.items()}
+        a = b.mtp_beam_args(R, W, V, 5, 3, 0.6, x_lg.data_ptr(), V, p["score"], p["length"], p["done"], p["score"], p["length"],
+                            p["done"], p["parent"], p["token"], None, 0)
+        ws = torch.empty(max(1, b.mtp_beam_select_workspace_size(a)), dtype=torch.uint8, device="cuda")
+        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        b.mtp_beam_select(a, torch.cuda.current_stream().cuda_stream)
+        for k, t in x.items():
+            assert np.array_equal(host(t), host(getattr(want, k))), k
+
+
+class Batch:
+    """One large call of every kind, whose plan, attention and selection need workspaces; inputs that can change."""
+
+    def __init__(self, seed, n=70, m=300, H=2, HQ=8, D=128, W=8, V=30000):
+        g = torch.Generator().manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        self.pages, self.W, self.V = n * 8 + m, W, V
+        kv = rng.integers(0, 100, n)
+        kv[0] = 16 * m - 40
+        self.length, self.add = dev(kv), dev(rng.integers(0, 4, n))
+        self.table = dev(tables(rng, kv + 4, m, self.pages))
+        self.T = 4 * n
+        self.pool = torch.randn((self.pages, 2, H, 16 * D), generator=g).bfloat16().cuda()
+        self.k, self.v = (torch.randn((self.T, H, D), generator=g).bfloat16().cuda() for _ in range(2))
+        self.q = torch.randn((self.T, HQ, D), generator=g).bfloat16().cuda()
+        self.out = torch.zeros((self.T, HQ, D), dtype=torch.bfloat16, device="cuda")
+        # a row alone over a long cache: its keys in runs
+        self.q1, self.one = self.q[:1].clone(), torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+        self.logits = torch.randn((2, W, V), generator=g).cuda()
+        self.score = torch.randn((2, W), generator=g).cuda()
+        self.zero = torch.zeros((2, W), dtype=torch.int32, device="cuda")
+
+    def run(self):
+        s = serving()
+        p = s.plan_pages(self.length, self.add, self.table, self.pages, self.T)
+        s.write_pages(self.pool, p.slots, self.k, self.v)
+        self.out.zero_()
+        s.attend_pages(self.pool, p.table, p.row_start, p.kv_len, self.q, max_kv=5000, out=self.out)
+        o1 = s.attend_pages(self.pool, p.table[:1], self.one, p.kv_len[:1], self.q1)
+        b = s.select_beams(self.logits, self.score, self.zero, self.zero, 1)
+        return (*p, self.out, o1, *b)
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_two_batches_at_once_on_two_streams():
+    a, b = Batch(1), Batch(2)
+    want_a, want_b = ([t.clone() for t in x.run()] for x in (a, b))
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got_a, got_b = [], []
+    for _ in range(6):
+        for st, x, got in ((s, a, got_a), (t, b, got_b)):
+            with torch.cuda.stream(st):
+                got.append([y.clone() for y in x.run()])
+    torch.cuda.synchronize()
+    assert all(same(g, want_a) for g in got_a) and all(same(g, want_b) for g in got_b)
+
+
+def test_two_graphs_and_eager_calls_in_turn():
+    """Two captured batches replayed in turn, and at once on two streams, with eager calls of a third and changed inputs
+    between; every replay against the eager result of the same inputs."""
+    x, y, z = Batch(3), Batch(4), Batch(5)
+    want_z = [t.clone() for t in z.run()]
+    graphs, outs = [], []
+    for b in (x, y):
+        b.run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(b.run())
+        graphs.append(g)
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for i in range(4):
+        for b in (x, y):
+            b.q.mul_(-1.1)
+            b.length[2:].copy_(torch.flip(b.length[2:], (0,)) // 2)
+            b.logits.copy_(b.logits.roll(77, 2))
+        want = [[t.clone() for t in b.run()] for b in (x, y)]
+        assert same(z.run(), want_z)
+        if i % 2:
+            torch.cuda.synchronize()
+            for st, g in zip(streams, graphs):
+                with torch.cuda.stream(st):
+                    g.replay()
+        else:
+            graphs[0].replay()
+            assert same(z.run(), want_z)
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        assert same(outs[0], want[0]) and same(outs[1], want[1]), i
