@@ -6,10 +6,11 @@
 // every row's lengths, fresh pages and running sums (one workgroup); every row
 // marks the pages that it keeps in a bitmap; every row takes its fresh pages by
 // rank among the clear bits and writes its table row, slots and positions.
-// Small plans run the three steps in one workgroup with the bitmap in LDS.
+// In all but the largest plans every row's workgroup finds out by itself what
+// the others keep, so that the three steps are one launch.
 // What bounds it: the chain of dependent loads (parent -> lengths -> table ->
-// bitmap) and the launches, not bytes: 256 rows of 250 pages, 0.5 MB, 14.7 us in
-// three launches; 8 rows of 229 pages 7.9 us in one.
+// marks) and the launches, not bytes: 8 rows of 229 pages 6.4 us, 256 beams of
+// 256 pages 14.6 us, 256 rows of 512 15.2 us in three launches.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -23,11 +24,13 @@ constexpr int PG = 16;                 // tokens per page
 constexpr int MAX_ROWS = 4096;
 constexpr int ROWS_T = 1024;           // threads of the step that takes every row
 constexpr int PLAN_T = 256;            // threads of the other two
-// One workgroup does all of it up to these sizes: table entries, bitmap words
-// (32 KB of LDS), rows (four for each wave) and tokens.  8 rows of 229 pages 8.3
-// us instead of 11.1 us in three launches, 32 of 256 10.4 and 10.9 us, 64 of 64
-// 11.2 and 11.3 us; 256 rows of 64 41 and 13.5 us, 10,400 tokens 13.5 and 10.9 us.
-constexpr int ONE_ENTRIES = 8192, ONE_WORDS = 8192, ONE_ROWS = 64, ONE_TOKENS = 4096;
+// One launch up to these sizes: table entries, pages (a byte of LDS each) and
+// rows (a workgroup each, so one or two a CU).  64 rows of 64 pages 7.4 us instead
+// of 11.3 us in three launches, 256 of 256 (beams) 14.6 and 14.8 us, 256 of 512
+// 20.6 and 15.2 us.  Workgroups of 256 threads, whose sums are shorter, for few
+// pieces of 64 entries: 8 rows of 229 pages 6.4 us, 7.8 us with 1024 threads; 256
+// rows of 16 pages 14.7 and 10.2 us.
+constexpr int ONE_ENTRIES = 1 << 16, ONE_PAGES = 1 << 17, ONE_ROWS = 256, FEW_PIECES = 64;
 
 // Row c of the plan: its parent, the parent's cached tokens, its new tokens
 // (the sign bit: its partly filled last page becomes a fresh one), and the
@@ -46,8 +49,7 @@ struct PlanWs {
 uint64_t plan_words(int num_pages) { return ((uint64_t)num_pages + 31) / 32; }
 
 bool plan_is_one(const mtp_plan_args& a) {
-    return a.n_rows <= ONE_ROWS && plan_words(a.num_pages) <= ONE_WORDS && (int64_t)a.n_rows * a.max_pages <= ONE_ENTRIES &&
-           a.max_tokens <= ONE_TOKENS;
+    return a.n_rows <= ONE_ROWS && a.num_pages <= ONE_PAGES && (int64_t)a.n_rows * a.max_pages <= ONE_ENTRIES;
 }
 
 uint64_t plan_carve(const mtp_plan_args& a, PlanWs* w) {
@@ -64,19 +66,20 @@ uint64_t plan_carve(const mtp_plan_args& a, PlanWs* w) {
 
 // Exclusive sums over the workgroup's NT threads; v becomes the sum of the
 // threads before, the result is the total.  buf: NT / 64 values of LDS.
-template <int NT>
-__device__ __forceinline__ int block_scan(int& v, int* buf) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, own = v;
-    int x = v;
+template <int NT, typename T>
+__device__ __forceinline__ T block_scan(T& v, T* buf) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const T own = v;
+    T x = v;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
+        const T y = __shfl_up(x, o);
         if (lane >= o) x += y;
     }
     __syncthreads();                   // (buf may still be read from the last call)
     if (lane == 63) buf[wave] = x;
     __syncthreads();
-    int before = 0, total = 0;
+    T before = 0, total = 0;
     for (int i = 0; i < NT / 64; ++i) {
         before += i < wave ? buf[i] : 0;
         total += buf[i];
@@ -85,15 +88,18 @@ __device__ __forceinline__ int block_scan(int& v, int* buf) {
     return total;
 }
 
-// Step 1 by one workgroup of NT threads: rows, row_start, kv_len, status.
-// low: n_rows words of LDS.
+// Step 1 by one workgroup of NT threads: r[k], row tid + NT k (empty behind the
+// last), and with `lead` row_start and kv_len; start: r[PER - 1]'s first token.
+// low: n_rows words of LDS.  The totals' low half counts fresh pages, the high
+// half new tokens (fewer than 2^31: the table holds fewer than 2^27 pages);
+// bad: this thread's rows outside their range.
 template <int NT, int PER>
-__device__ __forceinline__ void plan_rows(const mtp_plan_args& a, PlanRow* rows, int* low, int* buf) {
+__device__ __forceinline__ uint64_t plan_rows(const mtp_plan_args& a, PlanRow (&r)[PER], int* low, uint64_t* buf,
+                                              uint64_t& start, bool lead, int& bad) {
     const int tid = threadIdx.x, n = a.n_rows;
     for (int c = tid; c < n; c += NT) low[c] = 0x7fffffff;
     __syncthreads();
-    PlanRow r[PER];
-    int bad = 0;
+    bad = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int c = tid + NT * k;
@@ -112,32 +118,25 @@ __device__ __forceinline__ void plan_rows(const mtp_plan_args& a, PlanRow* rows,
         bad += ok ? 0 : 1;
     }
     __syncthreads();
-    int tokens = 0, pages = 0;         // of the slabs before (fewer than 2^31: the table holds fewer than 2^27 pages)
+    uint64_t sum = 0;                  // of the slabs before
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         if (NT * k >= n) break;        // uniform
         const int c = tid + NT * k;
         const bool in = c < n;
         if (in && a.parent && r[k].y % PG && low[r[k].x] != c) r[k].z |= (int)0x80000000;
-        int t = in ? row_new(r[k]) : 0, f = in ? row_need(r[k]) - row_kept(r[k]) : 0;
-        const int tt = block_scan<NT>(t, buf), ff = block_scan<NT>(f, buf);
-        if (in) {
-            r[k].w = pages + f;
-            rows[c] = r[k];
-            a.row_start[c] = tokens + t;
+        uint64_t v = in ? (uint64_t)row_new(r[k]) << 32 | (uint32_t)(row_need(r[k]) - row_kept(r[k])) : 0;
+        const uint64_t all = block_scan<NT>(v, buf);
+        r[k].w = (int)(uint32_t)(sum + v);
+        start = (sum + v) >> 32;
+        if (in && lead) {
+            a.row_start[c] = (int)start;
             a.kv_len[c] = r[k].y + row_new(r[k]);
         }
-        tokens += tt;
-        pages += ff;
+        sum += all;
     }
-    const int all_bad = block_scan<NT>(bad, buf);
-    if (tid == 0) {
-        a.row_start[n] = tokens;
-        a.status[0] = 0;
-        a.status[1] = all_bad;
-        a.status[2] = 0;
-        a.status[3] = 0;
-    }
+    if (lead && tid == 0) a.row_start[n] = (int)(sum >> 32);
+    return sum;
 }
 
 // Step 2 for row r by `nt` threads (this one is `i`).
@@ -172,17 +171,23 @@ __device__ __forceinline__ void plan_count(const uint32_t* bits, int num_pages, 
     __syncthreads();
 }
 
-// The page of rank k among the free ones, -1 past the last.
+// The run that holds the free page of rank k < before[NT]; k becomes its rank there.
 template <int NT>
-__device__ __forceinline__ int plan_page(const uint32_t* bits, int num_pages, int per, const int* before, int k) {
-    if (k >= before[NT]) return -1;
+__device__ __forceinline__ int plan_run(const int* before, int& k) {
     int lo = 0, hi = NT;               // before[lo] <= k < before[hi]
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (before[mid] <= k) lo = mid; else hi = mid;
     }
     k -= before[lo];
-    int i = lo * per;
+    return lo;
+}
+
+// The page of rank k among the free ones, -1 past the last.
+template <int NT>
+__device__ __forceinline__ int plan_page(const uint32_t* bits, int num_pages, int per, const int* before, int k) {
+    if (k >= before[NT]) return -1;
+    int i = plan_run<NT>(before, k) * per;
     uint32_t b = free_bits(bits, i, num_pages);
     while (k >= __popc(b)) {
         k -= __popc(b);
@@ -192,10 +197,10 @@ __device__ __forceinline__ int plan_page(const uint32_t* bits, int num_pages, in
     return i * 32 + __ffs(b) - 1;
 }
 
-// Step 3's table row by `nt` threads; the caller synchronises before plan_slots.
-template <int NT>
-__device__ __forceinline__ void plan_table(const mtp_plan_args& a, int c, const PlanRow& r, const uint32_t* bits, int per,
-                                           const int* before, int i, int nt) {
+// Step 3's table row by `nt` threads, page(k) the free page of rank k; the
+// caller synchronises before plan_slots.  The result: pages that there were not.
+template <typename F>
+__device__ __forceinline__ int plan_table(const mtp_plan_args& a, int c, const PlanRow& r, int i, int nt, F page) {
     const int keep = row_kept(r), need = row_need(r);
     const int32_t* src = a.table_in + (size_t)r.x * a.max_pages;
     int32_t* dst = a.table + (size_t)c * a.max_pages;
@@ -206,26 +211,22 @@ __device__ __forceinline__ void plan_table(const mtp_plan_args& a, int c, const 
             pg = src[j];
             if (pg < 0 || pg >= a.num_pages) pg = -1;
         } else if (j < need) {
-            pg = plan_page<NT>(bits, a.num_pages, per, before, r.w + (j - keep));
+            pg = page(r.w + (j - keep));
             missing += pg < 0 ? 1 : 0;
         }
         dst[j] = pg;
     }
-    if (missing) atomicAdd(&a.status[0], missing);
+    return missing;
 }
 
 // Slots, positions and the page copy of row c, its table row written.
 __device__ __forceinline__ void plan_slots(const mtp_plan_args& a, int c, const PlanRow& r, int64_t t0, int i, int nt) {
     const int32_t* dst = a.table + (size_t)c * a.max_pages;
-    int lost = 0;
-    for (int k = i; k < row_new(r); k += nt) {
-        const int64_t t = t0 + k;
-        if (t >= a.max_tokens) { ++lost; continue; }
+    for (int k = i; k < row_new(r) && t0 + k < a.max_tokens; k += nt) {
         const int pos = r.y + k, pg = dst[pos / PG];
-        a.slots[t] = pg >= 0 ? pg * PG + pos % PG : -1;
-        a.positions[t] = pos;
+        a.slots[t0 + k] = pg >= 0 ? pg * PG + pos % PG : -1;
+        a.positions[t0 + k] = pos;
     }
-    if (lost) atomicAdd(&a.status[3], lost);
     if (i == 0) {
         int s = -1, d = -1;
         if (row_moved(r)) {
@@ -246,10 +247,30 @@ __device__ __forceinline__ void plan_rest(const mtp_plan_args& a, int64_t tokens
     }
 }
 
+__device__ __forceinline__ int tokens_lost(const mtp_plan_args& a, uint64_t sum) {
+    return (int)max((int64_t)(sum >> 32) - a.max_tokens, (int64_t)0);
+}
+
 __global__ __launch_bounds__(ROWS_T) void plan_rows_kernel(mtp_plan_args a, PlanWs w) {
-    __shared__ int s_low[MAX_ROWS], s_buf[ROWS_T / 64];
+    __shared__ int s_low[MAX_ROWS];
+    __shared__ uint64_t s_buf[ROWS_T / 64];
     if (blockIdx.x == 0) {
-        plan_rows<ROWS_T, MAX_ROWS / ROWS_T>(a, w.rows, s_low, s_buf);
+        constexpr int PER = MAX_ROWS / ROWS_T;
+        PlanRow r[PER];
+        int bad;
+        uint64_t start;
+        const uint64_t sum = plan_rows<ROWS_T, PER>(a, r, s_low, s_buf, start, true, bad);
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if ((int)threadIdx.x + ROWS_T * k < a.n_rows) w.rows[threadIdx.x + ROWS_T * k] = r[k];
+        uint64_t b = bad;
+        const uint64_t all_bad = block_scan<ROWS_T>(b, s_buf);
+        if (threadIdx.x == 0) {
+            a.status[0] = 0;
+            a.status[1] = (int)all_bad;
+            a.status[2] = 0;
+            a.status[3] = tokens_lost(a, sum);
+        }
         return;
     }
     const int words = (a.num_pages + 31) / 32;
@@ -265,28 +286,112 @@ __global__ __launch_bounds__(PLAN_T) void plan_assign_kernel(mtp_plan_args a, Pl
     const int c = blockIdx.x;
     const PlanRow r = w.rows[c];
     if (row_need(r) > row_kept(r)) plan_count<PLAN_T>(w.bits, a.num_pages, per, s_before, s_buf);
-    plan_table<PLAN_T>(a, c, r, w.bits, per, s_before, threadIdx.x, PLAN_T);
+    const int missing = plan_table(a, c, r, threadIdx.x, PLAN_T,
+                                   [&](int k) { return plan_page<PLAN_T>(w.bits, a.num_pages, per, s_before, k); });
+    if (missing) atomicAdd(&a.status[0], missing);
     __syncthreads();
     plan_slots(a, c, r, a.row_start[c], threadIdx.x, PLAN_T);
     plan_rest(a, a.row_start[a.n_rows], (int64_t)c * PLAN_T + threadIdx.x, (int64_t)gridDim.x * PLAN_T);
 }
 
-// All three steps by one workgroup, a wave per row.
-__global__ __launch_bounds__(ROWS_T) void plan_one_kernel(mtp_plan_args a, int per) {
-    __shared__ uint32_t s_bits[ONE_WORDS];
-    __shared__ PlanRow s_rows[ONE_ROWS];
-    __shared__ int s_low[ONE_ROWS], s_buf[ROWS_T / 64], s_before[ROWS_T + 1];
-    const int words = (a.num_pages + 31) / 32, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < words; i += ROWS_T) s_bits[i] = 0u;
-    plan_rows<ROWS_T, 1>(a, s_rows, s_low, s_buf);
+// Free pages among the 16 of a quad, and the page of rank k among those of the
+// quads from i on (there is one).
+__device__ __forceinline__ int quad_free(const uint4& x) {
+    return 16 - __popc(x.x) - __popc(x.y) - __popc(x.z) - __popc(x.w);
+}
+__device__ __forceinline__ int free_byte(const uint4* used, int i, int k) {
+    uint4 x = used[i];
+    for (int f = quad_free(x); k >= f; f = quad_free(x)) {
+        k -= f;
+        x = used[++i];
+    }
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t b = ~w[0] & 0x01010101u;
+    int at = 0;
+#pragma unroll
+    for (int q = 1; q < 4; ++q)
+        if (k >= __popc(b)) {
+            k -= __popc(b);
+            b = ~w[q] & 0x01010101u;
+            at = 4 * q;
+        }
+    for (; k > 0; --k) b &= b - 1;
+    return 16 * i + at + ((__ffs(b) - 1) >> 3);
+}
+
+// All three steps by a workgroup per row: each takes every row's lengths and,
+// where its own row (or the status, workgroup 0's) needs to know the free
+// pages, marks what every row keeps in LDS, a byte a page (stores without
+// atomics: neighbouring pages, which a row mostly has, would queue up at the
+// words of a bitmap).
+template <int NT>
+__global__ __launch_bounds__(NT) void plan_alone_kernel(mtp_plan_args a) {
+    constexpr int FLY = 4;             // pieces in flight per wave
+    __shared__ uint4 s_used[ONE_PAGES / 16];
+    __shared__ int2 s_piece[ONE_ENTRIES / 64 + ONE_ROWS];      // up to 64 kept entries of a row: first in table_in, number
+    __shared__ PlanRow s_own;
+    __shared__ int s_low[ONE_ROWS], s_buf[NT / 64], s_before[NT + 1], s_start, s_bad[2];
+    __shared__ uint64_t s_sum[NT / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = blockIdx.x;
+    const bool lead = c == 0;
+    const int quads = (a.num_pages + 15) / 16, per = (quads + NT - 1) / NT;
+    if (tid < 2) s_bad[tid] = 0;
+    int bad;
+    uint64_t start;
+    PlanRow mine[1];
+    const uint64_t sum = plan_rows<NT, 1>(a, mine, s_low, s_sum, start, lead, bad);
+    if (lead && bad) atomicAdd(&s_bad[0], bad);
+    if (tid == c) { s_own = mine[0]; s_start = (int)start; }
+    const int kept = tid < a.n_rows ? row_kept(mine[0]) : 0;
+    int at = (kept + 63) / 64;
+    const int pieces = block_scan<NT>(at, s_buf);
+    const PlanRow r = s_own;
+    const bool fresh = lead || row_need(r) > row_kept(r);      // uniform
+    if (fresh) {
+        for (int j = 0; j < kept; j += 64) s_piece[at++] = make_int2(mine[0].x * a.max_pages + j, min(kept - j, 64));
+        for (int i = tid; i < quads; i += NT) s_used[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+        uint8_t* used = reinterpret_cast<uint8_t*>(s_used);
+        bad = 0;
+        for (int u0 = wave; u0 < pieces; u0 += NT / 64 * FLY) {
+            int pg[FLY], n[FLY];
+#pragma unroll
+            for (int k = 0; k < FLY; ++k) {
+                const int u = u0 + NT / 64 * k;
+                const int2 x = s_piece[min(u, pieces - 1)];
+                n[k] = u < pieces ? x.y : 0;
+                pg[k] = lane < n[k] ? a.table_in[x.x + lane] : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < FLY; ++k) {
+                if ((uint32_t)pg[k] < (uint32_t)a.num_pages) used[pg[k]] = 1;
+                else bad += lane < n[k] ? 1 : 0;
+            }
+        }
+        if (lead && bad) atomicAdd(&s_bad[1], bad);
+        if (tid < quads * 16 - a.num_pages) used[a.num_pages + tid] = 1;
+        __syncthreads();
+        const int q0 = min(tid * per, quads), q1 = min(q0 + per, quads);
+        int cnt = 0;
+        for (int i = q0; i < q1; ++i) cnt += quad_free(s_used[i]);
+        const int all = block_scan<NT>(cnt, s_buf);
+        s_before[tid] = cnt;
+        if (tid == 0) s_before[NT] = all;
+        __syncthreads();
+    }
+    if (lead && tid == 0) {
+        a.status[0] = max((int)(uint32_t)sum - s_before[NT], 0);
+        a.status[1] = s_bad[0];
+        a.status[2] = s_bad[1];
+        a.status[3] = tokens_lost(a, sum);
+    }
+    plan_table(a, c, r, tid, NT, [&](int k) {
+        if (k >= s_before[NT]) return -1;
+        return free_byte(s_used, plan_run<NT>(s_before, k) * per, k);
+    });
     __syncthreads();
-    for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_mark(a, s_rows[c], s_bits, lane, 64);
-    __syncthreads();
-    plan_count<ROWS_T>(s_bits, a.num_pages, per, s_before, s_buf);
-    for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_table<ROWS_T>(a, c, s_rows[c], s_bits, per, s_before, lane, 64);
-    __syncthreads();
-    for (int c = wave; c < a.n_rows; c += ROWS_T / 64) plan_slots(a, c, s_rows[c], a.row_start[c], lane, 64);
-    plan_rest(a, a.row_start[a.n_rows], threadIdx.x, ROWS_T);
+    plan_slots(a, c, r, s_start, tid, NT);
+    plan_rest(a, sum >> 32, (int64_t)c * NT + tid, (int64_t)gridDim.x * NT);
 }
 
 bool aligned(const void* p, uintptr_t n) { return p && ((uintptr_t)p & (n - 1)) == 0; }
@@ -450,7 +555,10 @@ int mtp_pages_plan(const mtp_plan_args* args, void* hip_stream) {
     hipStream_t st = (hipStream_t)hip_stream;
     const int words = (int)plan_words(a.num_pages);
     if (need == 0) {
-        hipLaunchKernelGGL(plan_one_kernel, dim3(1), dim3(ROWS_T), 0, st, a, (words + ROWS_T - 1) / ROWS_T);
+        if (a.n_rows * ((a.max_pages + 63) / 64) <= FEW_PIECES)
+            hipLaunchKernelGGL(plan_alone_kernel<256>, dim3(a.n_rows), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL(plan_alone_kernel<1024>, dim3(a.n_rows), dim3(1024), 0, st, a);
         return launched();
     }
     const int cb = (words + ROWS_T * 4 - 1) / (ROWS_T * 4);

@@ -35,7 +35,7 @@ _DTYPE = {torch.float32: _b.MTP_DTYPE_F32, torch.bfloat16: _b.MTP_DTYPE_BF16}
 
 
 class PagePlan(NamedTuple):
-    """int32 tensors; the fields of mtp_plan_args."""
+    """int32 tensors; the fields of mtp_plan_args (views of one allocation)."""
     table: torch.Tensor       # [rows, max_pages]
     row_start: torch.Tensor   # [rows + 1]
     kv_len: torch.Tensor      # [rows]
@@ -144,25 +144,25 @@ def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num
     p_len, p_add = _ints(length, "length", (n,), dev), _ints(add, "add", (n,), dev)
     p_in = _ints(table, "table", (n, m), dev)
     p_par = None if parent is None else _ints(parent, "parent", (n,), dev)
-    i32 = torch.int32
-    new = torch.empty_like(table) if out_table is None else out_table
-    p_new = _ints(new, "out_table", (n, m), dev)
+    # one allocation for the outputs, cut once (views cost the call more than its checks); the table first
+    own = n * m if out_table is None else 0
+    cut = (own, 2 * n, n, n + 1, 4, max_tokens, max_tokens)
+    new, copies, kv_len, row_start, status, slots, positions = torch.split_with_sizes(
+        torch.empty(sum(cut), dtype=torch.int32, device=dev), cut)
+    new = new.view(n, m) if out_table is None else out_table
+    p_new = new.data_ptr() if out_table is None else _ints(new, "out_table", (n, m), dev)
     _need(p_par is None or p_new != p_in or n == 0, "out_table: not the table itself where rows have parents")
-    # one allocation for the small outputs: starts, lengths, copies, status
-    small = torch.empty(4 * n + 5, dtype=i32, device=dev)
-    tok = torch.empty((2, max_tokens), dtype=i32, device=dev)
-    base = small.data_ptr()
+    base, tok = status.data_ptr() - 4 * (4 * n + 1), slots.data_ptr()
     args = _b.mtp_plan_args(n, m, num_pages, max_tokens, p_par, p_len, p_add, p_in, p_new,
-                            base + 4 * 3 * n, base + 4 * 2 * n, tok.data_ptr() or None,
-                            tok.data_ptr() + 4 * max_tokens if max_tokens else None, base, base + 4 * (4 * n + 1), None, 0)
+                            base + 4 * 3 * n, base + 4 * 2 * n, tok, tok + 4 * max_tokens, base, base + 4 * (4 * n + 1), None, 0)
     ws = _workspace(_b.mtp_pages_plan_workspace_size, args, dev)
     if n == 0:
-        small.zero_()
-        tok.fill_(-1)
+        row_start.zero_()
+        status.zero_()
+        slots.fill_(-1)
+        positions.fill_(-1)
     else:
         _launch(_b.mtp_pages_plan, args, dev)
-    copies, kv_len, row_start, status = small.split((2 * n, n, n + 1, 4))
-    slots, positions = tok.unbind(0)
     return PagePlan(new, row_start, kv_len, slots, positions, copies.view(n, 2), status)
 
 

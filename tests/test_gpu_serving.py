@@ -55,7 +55,8 @@ def check_plan(length, add, table, pages, max_tokens, parent=None, in_place=Fals
 
 
 @pytest.mark.parametrize("n,m,hi,add_hi", [(1, 1, 0, 1), (1, 3, 20, 20), (7, 5, 60, 20), (8, 229, 3600, 4),
-                                           (64, 40, 500, 130), (257, 17, 255, 17), (4096, 2, 20, 12)])
+                                           (64, 40, 500, 130), (257, 17, 255, 17), (4096, 2, 20, 12),
+                                           (256, 4, 60, 3), (200, 61, 900, 9), (70, 1000, 15000, 700)])
 @pytest.mark.parametrize("beams", [False, True])
 def test_plan(n, m, hi, add_hi, beams):
     rng = np.random.default_rng(n * 1000 + m)
@@ -76,7 +77,7 @@ def test_plan(n, m, hi, add_hi, beams):
         check_plan(length, add, table, pages, int(add.sum()), in_place=True)
 
 
-@pytest.mark.parametrize("pages", [1, 31, 32, 33, 64, 1000, 70001])
+@pytest.mark.parametrize("pages", [1, 15, 16, 17, 31, 32, 33, 64, 1000, 4097, 70001, 131072, 131073, 300001])
 def test_plan_hands_out_the_lowest_free_pages(pages):
     rng = np.random.default_rng(pages)
     m = 40

@@ -25,7 +25,7 @@ BAD_CACHE = [dict(pool=0), dict(pool=4104), dict(dtype=2), dict(dtype=-1), dict(
 
 def _plan(**kw):
     from paper_2410_13839_amd import binding as b
-    a = b.mtp_plan_args(2, 5000, 64, 8, None, 256, 512, 768, 1024, 2048, 2304, 2560, 2816, 3136, 3328, 4096, 1 << 20)
+    a = b.mtp_plan_args(2, 50000, 64, 8, None, 256, 512, 768, 1024, 2048, 2304, 2560, 2816, 3136, 3328, 4096, 1 << 20)
     for k, v in kw.items():
         setattr(a, k, v)
     return a
