@@ -744,13 +744,19 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
         if (hh == 0) g.ml[slot] = make_float2(m, l);
     } else {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16_t* op = (bf16_t*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + 4 * hh;
+        bf16_t* op = (bf16_t*)a.out + (int64_t)(t.t0 + qr / g.gs) * a.out_stride + (hk * group + h0 + qr % g.gs) * D + 8 * hh;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<uint2*>(op + 32 * dt + 2 * i) =
-                    make_uint2(pk2(o[dt][i] * inv, o[dt][i + 1] * inv), pk2(o[dt][i + 2] * inv, o[dt][i + 3] * inv));
+            for (int i = 0; i < 16; i += 8) {
+                // of 16 dimensions lane h has 4 h .. + 3 and 8 + 4 h .. + 3; exchanged, 8 h .. + 7
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = pk2(o[dt][i + 2 * k] * inv, o[dt][i + 2 * k + 1] * inv);
+                const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+                const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                *reinterpret_cast<uint4*>(op + 32 * dt + 2 * i) = make_uint4(x[0], y[0], x[1], y[1]);
+            }
     }
 }
 
