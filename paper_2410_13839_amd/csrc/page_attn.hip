@@ -469,9 +469,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
 // exponentials (software pipelining) measured the same and cost registers; so
 // did a third block in LDS, raised priority around the products, and tiles
 // dealt longest first.  Measured, 32 query heads on 8 KV heads of 128: chunks of
-// 512 tokens over 8192 keys 314 us (848 TFLOP/s), whole prompts of 4096 623 us
-// (880), chunks of up to 512 over 2048 to 8192 keys 213 us (685: the longest
-// rows' workgroups finish last); 16 heads of 64, 450-token prompts 23.3 us.
+// 512 tokens over 8192 keys 302 us (880 TFLOP/s), whole prompts of 4096 620 us
+// (887), chunks of up to 512 over 2048 to 8192 keys 217 us (672: the longest
+// rows' workgroups finish last); 16 heads of 64, 450-token prompts 23.1 us.
+// Pages of a part-seen block that no row of the wave sees are left out, scores
+// and values: those chunks 302 us instead of 314 us.
 // Head dim 64 with four workgroups a CU instead of three: 230 -> 199 us.
 constexpr int TR = 128;                          // query rows of a tile
 constexpr int KB = 64;                           // keys of a block
@@ -643,7 +645,18 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
     auto edge = [&](int buf, int kb, int bad) {
         f32x16_t s[2];
         bf16x8_t p[4];
-        scores(buf, s);
+        const int end = min(k1, whi);            // no row of the wave sees keys from here on, nor before wlo
+        if (kb + 32 < end) {
+            scores(buf, s);
+        } else {
+            const bf16_t* K = s_k[buf] + krow * D;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    *reinterpret_cast<const bf16x8_t*>(K + ((2 * j + hh) ^ ksw) * 8), q[j], s[0], 0, 0, 0);
+        }
         // register i of tile tt: key kb + 32 tt + 16 (i / 8) + 8 hh + i % 8, page 2 tt + i / 8 of the block
         const int slo = max(rlo, t.lo) - (kb + 8 * hh);
         const unsigned span = max(0, min(rhi, k1) - max(rlo, t.lo));
@@ -677,9 +690,20 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
         const bool any_odd = __any(odd);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
+            // the page's first key: uniform, as the ways below are (with head dim 64 there are no registers for the
+            // second: 16 rows of 450 tokens 34 us with it, 28.5 us without)
+            const int ka = kb + 16 * u;
+            if ((bad >> u & 1) || ka >= end || ka + PG <= wlo) continue;
+            if (D == 128 && ka >= t.lo && ka + PG <= k1 && !any_odd) {
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        *reinterpret_cast<const bf16x8_t*>(V + u * PG * D + 32 * dt * PG), p[u], o[dt], 0, 0, 0);
+                continue;
+            }
             uint32_t in[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) in[j] = bad >> u & 1 ? 0u : inside2(kb + 16 * u + 8 * hh + 2 * j, t.lo, k1);
+            for (int j = 0; j < 4; ++j) in[j] = inside2(ka + 8 * hh + 2 * j, t.lo, k1);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt) {
                 uint4 v = *reinterpret_cast<const uint4*>(V + u * PG * D + 32 * dt * PG);
