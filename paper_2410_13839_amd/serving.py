@@ -208,7 +208,7 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
     _need(table.dim() == 2, "table: [rows, max_pages]")
     n, m = table.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = torch.empty_like(q)                # (contiguous, as a token's heads are)
         os = q.shape[1] * dim
     else:
         _need(out.shape == q.shape, "out: q's shape")
