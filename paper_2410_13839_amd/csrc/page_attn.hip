@@ -53,6 +53,27 @@ __device__ __forceinline__ int start_of(const mtp_attention_args& a, int c) {
     return max(0, min(a.row_start[c], a.n_tokens));
 }
 
+// Tile `local` of row c, whose tokens are [s, e).
+__device__ __forceinline__ AttnTile tile_at(const mtp_attention_args& a, const AttnGeo& g, int c, int s, int e, int kv,
+                                            int local) {
+    AttnTile t;
+    t.c = c;
+    t.t0 = s + local * g.tt;
+    t.nt = local < 0 ? 0 : max(0, min(g.tt, e - t.t0));
+    t.kv = kv;
+    t.pos0 = t.kv - (e - s) + (t.t0 - s);
+    t.lo = 0;
+    t.hi = t.kv;
+    if (a.mode == MTP_ATTN_CAUSAL) {
+        t.hi = max(0, min(t.kv, t.pos0 + t.nt));
+        if (a.window > 0) t.lo = max(0, t.pos0 - a.window + 1);
+    }
+    return t;
+}
+__device__ __forceinline__ int keys_of(const mtp_attention_args& a, int c) {
+    return max(0, min(a.kv_len[c], PG * a.max_pages));
+}
+
 // The tile's row, found by the whole wave, 64 candidates a round; uniform.
 __device__ __forceinline__ AttnTile find_tile(const mtp_attention_args& a, const AttnGeo& g, int tile) {
     const int lane = threadIdx.x & 63;
@@ -64,21 +85,44 @@ __device__ __forceinline__ AttnTile find_tile(const mtp_attention_args& a, const
         lo += (k - 1) * step;
         n = min(step, n - (k - 1) * step);
     }
-    AttnTile t;
-    t.c = __builtin_amdgcn_readfirstlane(lo);
-    const int s = start_of(a, t.c), e = start_of(a, t.c + 1);
-    t.t0 = s + (tile - (s / g.tt + t.c)) * g.tt;
-    t.nt = max(0, min(g.tt, e - t.t0));
-    if (t.t0 < s) t.nt = 0;
-    t.kv = max(0, min(a.kv_len[t.c], PG * a.max_pages));
-    t.pos0 = t.kv - (e - s) + (t.t0 - s);
-    t.lo = 0;
-    t.hi = t.kv;
-    if (a.mode == MTP_ATTN_CAUSAL) {
-        t.hi = max(0, min(t.kv, t.pos0 + t.nt));
-        if (a.window > 0) t.lo = max(0, t.pos0 - a.window + 1);
+    const int c = __builtin_amdgcn_readfirstlane(lo);
+    const int s = start_of(a, c), e = start_of(a, c + 1);
+    return tile_at(a, g, c, s, e, keys_of(a, c), tile - (s / g.tt + c));
+}
+
+// Work item u of a head: a tile and a run of its keys; the whole runs of every
+// row first, then the rows' rests, the longest first, and nothing (no tokens)
+// behind them: workgroups start in this order, so that the last ones to start
+// are short.  Up to 64 rows, a lane each; beyond, tiles in order, run by run.
+__device__ __forceinline__ AttnTile find_item(const mtp_attention_args& a, const AttnGeo& g, int u, int& tile, int& split) {
+    if (a.n_rows > 64) {
+        split = u / g.n_tiles;
+        tile = u - split * g.n_tiles;
+        return find_tile(a, g, tile);
     }
-    return t;
+    const int lane = threadIdx.x & 63, c = min(lane, a.n_rows - 1);
+    const int s = start_of(a, c), e = start_of(a, c + 1), kv = keys_of(a, c);
+    const int count = lane < a.n_rows && e > s ? (e - s + g.tt - 1) / g.tt : 0;
+    const int whole = min(kv / g.split_len, g.n_splits), rest = whole < g.n_splits ? kv - whole * g.split_len : -1;
+    const int c0 = count * whole, c1 = rest >= 0 ? count : 0;
+    int b0 = 0, b1 = 0, all0 = 0;                // items before this lane's whole runs and before its rest
+    for (int k = 0; k < a.n_rows; ++k) {
+        const int k0 = __builtin_amdgcn_readlane(c0, k), k1 = __builtin_amdgcn_readlane(c1, k);
+        const int kr = __builtin_amdgcn_readlane(rest, k);
+        all0 += k0;
+        b0 += k < lane ? k0 : 0;
+        b1 += kr > rest || (kr == rest && k < lane) ? k1 : 0;
+    }
+    const bool first = u < all0;
+    const int at = first ? u - b0 : u - all0 - b1, n = first ? c0 : c1;
+    const uint64_t hit = __ballot(at >= 0 && at < n);
+    const int l = hit ? __ffsll((unsigned long long)hit) - 1 : 0;
+    const int rs = __builtin_amdgcn_readlane(s, l), rc = max(1, __builtin_amdgcn_readlane(count, l));
+    const int i = __builtin_amdgcn_readlane(at, l), run = first ? i / rc : __builtin_amdgcn_readlane(whole, l);
+    const int local = first ? i - run * rc : i;
+    split = run;
+    tile = rs / g.tt + l + local;
+    return tile_at(a, g, l, rs, __builtin_amdgcn_readlane(e, l), __builtin_amdgcn_readlane(kv, l), hit ? local : -1);
 }
 
 // The keys [k0, k1) of run `split`, and the number of live runs (at least 1;
@@ -489,13 +533,11 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qc = lane & 31, hh = lane >> 5;
     const int H = a.cache.n_kv_heads, HB = H * g.hb;
-    // the tiles of one head and run on one XCD (workgroups are dealt to the 8 XCDs in turn), whose L2 then holds
-    // their keys
-    const unsigned total = (unsigned)g.n_tiles * HB * g.n_splits, chunk = (total + 7) / 8;
-    const unsigned wi = (blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= chunk || wi >= total) return;
-    const int tile = wi % g.n_tiles, hs = wi / g.n_tiles, split = hs % g.n_splits, hbi = hs / g.n_splits, hk = hbi / g.hb;
-    const AttnTile t = find_tile(a, g, tile);
+    // heads fastest: workgroups are dealt to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD has its own,
+    // whose keys its L2 then holds
+    const int u = blockIdx.x / HB, hbi = blockIdx.x - u * HB, hk = hbi / g.hb;
+    int tile, split;
+    const AttnTile t = find_item(a, g, u, tile, split);
     if (t.nt == 0) return;
     int k0, k1;
     const int live = runs_of(g, t, split, k0, k1);
@@ -889,7 +931,7 @@ int rows_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
 template <int D>
 int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
-    hipLaunchKernelGGL((attn_tile_kernel<D>), dim3((work * g.n_splits + 7) / 8 * 8), dim3(256), 0, st, a, g);
+    hipLaunchKernelGGL((attn_tile_kernel<D>), dim3(work * g.n_splits), dim3(256), 0, st, a, g);
     join_go<bf16_t, D, TR>(st, a, g, work);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
