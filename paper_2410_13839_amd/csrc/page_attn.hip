@@ -39,6 +39,7 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 // leaves partial sums for a second launch.
 struct AttnGeo {
     int gs, hb, tt, n_tiles, n_splits, split_len;
+    int sorted;                // workgroups in the order of find_item
     float* acc;                // [n_tiles * heads * hb][n_splits][tile rows][D]
     float2* ml;                // [...][tile rows] reference and sum
 };
@@ -52,6 +53,8 @@ struct AttnTile {
 __device__ __forceinline__ int start_of(const mtp_attention_args& a, int c) {
     return max(0, min(a.row_start[c], a.n_tokens));
 }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Tile `local` of row c, whose tokens are [s, e).
 __device__ __forceinline__ AttnTile tile_at(const mtp_attention_args& a, const AttnGeo& g, int c, int s, int e, int kv,
@@ -93,10 +96,10 @@ __device__ __forceinline__ AttnTile find_tile(const mtp_attention_args& a, const
 // Work item u of a head: a tile and a run of its keys; the whole runs of every
 // row first, then the rows' rests, the longest first, and nothing (no tokens)
 // behind them: workgroups start in this order, so that the last ones to start
-// are short.  Up to 64 rows, a lane each; beyond, tiles in order, run by run.
+// are short.  A lane each row; unsorted, tiles in order, run by run.
 __device__ __forceinline__ AttnTile find_item(const mtp_attention_args& a, const AttnGeo& g, int u, int& tile, int& split) {
-    if (a.n_rows > 64) {
-        split = u / g.n_tiles;
+    if (!g.sorted) {
+        split = uniform(u / g.n_tiles);
         tile = u - split * g.n_tiles;
         return find_tile(a, g, tile);
     }
@@ -120,9 +123,10 @@ __device__ __forceinline__ AttnTile find_item(const mtp_attention_args& a, const
     const int rs = __builtin_amdgcn_readlane(s, l), rc = max(1, __builtin_amdgcn_readlane(count, l));
     const int i = __builtin_amdgcn_readlane(at, l), run = first ? i / rc : __builtin_amdgcn_readlane(whole, l);
     const int local = first ? i - run * rc : i;
-    split = run;
-    tile = rs / g.tt + l + local;
-    return tile_at(a, g, l, rs, __builtin_amdgcn_readlane(e, l), __builtin_amdgcn_readlane(kv, l), hit ? local : -1);
+    split = uniform(run);
+    tile = uniform(rs / g.tt + l + local);
+    return tile_at(a, g, uniform(l), rs, __builtin_amdgcn_readlane(e, l), __builtin_amdgcn_readlane(kv, l),
+                   uniform(hit ? local : -1));
 }
 
 // The keys [k0, k1) of run `split`, and the number of live runs (at least 1;
@@ -185,11 +189,10 @@ __device__ __forceinline__ uint32_t inside2(int y, int lo, int hi) {
 // tile dt is dimension (D / 16) r + dt, all 16-byte loads again.
 //
 // What bounds it: HBM where there are many keys (32 single tokens over 512 to
-// 16,384 keys, 1.1 GB: 220 us, 5.0 TB/s, what a large copy reaches), the chain
-// of loads lengths -> table -> keys and the second launch where there are few (4
-// tokens over 1075 keys of 16 heads 9.0 us; with 16 waves a head in one launch
-// 11.8 us: a CU alone draws 25 to 50 GB/s).  A lookup of all rows' lengths in one
-// round of loads cost registers and measured slower.
+// 16,384 keys, 1.1 GB: 210 us, 5.3 TB/s, what a large copy reaches; 220 us with
+// the runs in the rows' order), the chain of loads lengths -> table -> keys and
+// the second launch where there are few (4 tokens over 1075 keys of 16 heads 8.8
+// us; with 16 waves a head in one launch 11.8 us: a CU alone draws 25 to 50 GB/s).
 constexpr int NW = 4;
 
 template <typename T, int D>
@@ -244,12 +247,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, gr = lane >> 4;
     const int H = a.cache.n_kv_heads, HB = H * g.hb;
-    const int tile = blockIdx.x / HB, hbi = blockIdx.x - tile * HB, hk = hbi / g.hb;
-    const AttnTile t = find_tile(a, g, tile);
+    const int u = uniform(blockIdx.x / HB), hbi = blockIdx.x - u * HB, hk = hbi / g.hb;
+    int tile, split;
+    const AttnTile t = find_item(a, g, u, tile, split);
     if (t.nt == 0) return;
     int k0, k1;
-    const int live = runs_of(g, t, blockIdx.y, k0, k1);
-    if ((int)blockIdx.y >= live) return;
+    const int live = runs_of(g, t, split, k0, k1);
+    if (split >= live) return;
 
     const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs;      // first head of the block in its group
     const int heads = min(g.gs, group - h0), rows = t.nt * g.gs;
@@ -453,7 +457,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
         }
     }
     __syncthreads();
-    const size_t slot = ((size_t)blockIdx.x * g.n_splits + blockIdx.y) * QR;
+    const size_t slot = (((size_t)tile * HB + hbi) * g.n_splits + split) * QR;
     for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * NW) {
         const int qr = i / (D / 4), d = (i - qr * (D / 4)) * 4;
         if (qr % g.gs >= heads) continue;
@@ -535,7 +539,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
     const int H = a.cache.n_kv_heads, HB = H * g.hb;
     // heads fastest: workgroups are dealt to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD has its own,
     // whose keys its L2 then holds
-    const int u = blockIdx.x / HB, hbi = blockIdx.x - u * HB, hk = hbi / g.hb;
+    const int u = uniform(blockIdx.x / HB), hbi = blockIdx.x - u * HB, hk = hbi / g.hb;
     int tile, split;
     const AttnTile t = find_item(a, g, u, tile, split);
     if (t.nt == 0) return;
@@ -923,7 +927,7 @@ void join_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g, unsi
 template <typename T, int D>
 int rows_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
-    hipLaunchKernelGGL((attn_rows_kernel<T, D>), dim3(work, g.n_splits), dim3(64 * NW), 0, st, a, g);
+    hipLaunchKernelGGL((attn_rows_kernel<T, D>), dim3(work * g.n_splits), dim3(64 * NW), 0, st, a, g);
     join_go<T, D, 16>(st, a, g, work);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
@@ -953,20 +957,34 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     x.wide = a.cache.dtype == MTP_DTYPE_BF16 && (int64_t)a.n_tokens * x.g.gs >= (d128 ? 8ll : 64ll) * a.n_rows;
     const int rt = x.wide ? TR : 16;
     x.g.tt = rt / x.g.gs;
-    x.g.n_tiles = a.n_tokens / x.g.tt + a.n_rows;
+    x.g.n_tiles = a.n_rows == 1 ? (a.n_tokens + x.g.tt - 1) / x.g.tt : a.n_tokens / x.g.tt + a.n_rows;
     const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
-    // Runs of the keys: as many workgroups as the CUs hold at once (wide: two a CU with head dim 128, three with 64; four
-    // fit, but 128 tokens over 8000 keys take 31 us then, 28.5 us with three), no run shorter than 256 keys (narrow:
-    // 128).  Narrow: keys below 512 stay whole (400 keys of 16 heads 7.4 us whole, 8.1 us in three runs), so do tiles that
-    // fill three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us whole, 38 us in three), at most 32
-    // runs (16,000 keys of 8 KV heads 26 us, 33 us in 64).  Of a long cache runs of 2560 keys, which even out ragged
-    // rows, while the tiles are few and part full (32 rows of up to 16,384 keys: 4 query rows each 257 us in two runs, 220
-    // us in six; 8 each, wide, 269 and 212 us; full tiles, 512 of them over 8192 keys: 314 us whole, 365 us in three).
+    // Sorting costs a workgroup some 25 ns a row, more than it gives few query rows on short keys (40 single tokens over
+    // up to 700 keys, 16 heads: 19.1 us in the tiles' order, 20.1 us sorted; 32 over up to 1190 keys 27.8 and 27.0 us;
+    // wide, 16 rows of 300 to 750 tokens over up to 150: 21.4 and 20.5 us).
+    x.g.sorted = a.n_rows > 1 && a.n_rows <= 64 && (x.wide || kv >= 20ll * a.n_rows);
+    // Runs of the keys.  Wide: 512 workgroups, two a CU, as many as fit with head dim 128; 768 with head dim 64 (16 rows
+    // of 128 tokens: 45.4 us, 52 us with 1152) and where the tiles are part full (16 rows of 8 query rows over 1000 to
+    // 4000 keys, head dim 128: 43 us, 49 us with 512).  With
+    // head dim 64 and full tiles up to four runs, for the sorted order's sake (6 rows of 300 to 512 tokens over up to
+    // 8192 keys: two runs 93 us, three 79; 3 rows of 64 to 600 over up to 6000: four 51 us, five 60).  No run shorter
+    // than 256 keys.  Narrow: 512 workgroups, runs of 128 keys at least, at most 32 of them (16,000 keys of 8 KV heads 26
+    // us, 33 us in 64); whole below 512 keys (400 keys of 16 heads 7.4 us, 8.1 us in three runs) and where the tiles fill
+    // three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us, 38 us in three).  But runs of 1024 keys of
+    // long caches, which even out ragged rows, while the tiles are part full, up to ten workgroups a CU (8 rows of 32
+    // tokens over 3000 to 8000 keys, 8 heads of 64: 54 us whole, 34 us in seven; 32 single tokens over up to 16,384: 242
+    // us in two, 210 in eight, 225 in twelve).
     const bool few = (int64_t)a.n_tokens * x.g.gs <= (int64_t)TR * a.n_rows;
     int64_t n;
-    if (x.wide) n = std::min<int64_t>(((d128 ? 512 : 768) + work - 1) / work, kv / 256);
-    else n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>((512 + work - 1) / work, kv / 128), 32);
-    if (kv >= 8192 && few) n = std::max<int64_t>(n, std::min<int64_t>(kv / 2560, 4096 / work));
+    auto runs = [&](int64_t workgroups) { return (workgroups + work - 1) / work; };
+    if (x.wide) {
+        n = runs(few || !d128 ? 768 : 512);
+        if (!few && !d128) n = std::max<int64_t>(n, std::min<int64_t>(runs(1152), 4));
+        n = std::min<int64_t>(n, kv / 256);
+    } else {
+        n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>(runs(512), kv / 128), 32);
+        if (kv >= 4096 && few) n = std::max<int64_t>(n, std::min<int64_t>(kv / 1024, 2560 / work));
+    }
     n = std::max<int64_t>(1, std::min<int64_t>(n, MAX_RUNS));
     x.g.n_splits = (int)n;
     x.g.split_len = (int)(((kv + n - 1) / n + KB - 1) / KB * KB);
