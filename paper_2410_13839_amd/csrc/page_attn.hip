@@ -515,13 +515,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
 // conversions; counters show each busy 42 to 44% of the time, the two waves of a
 // SIMD overlapping little.  Forming the next block's scores during the
 // exponentials (software pipelining) measured the same and cost registers; so
-// did a third block in LDS, raised priority around the products, and tiles
-// dealt longest first.  Measured, 32 query heads on 8 KV heads of 128: chunks of
-// 512 tokens over 8192 keys 302 us (880 TFLOP/s), whole prompts of 4096 620 us
-// (887), chunks of up to 512 over 2048 to 8192 keys 217 us (672: the longest
-// rows' workgroups finish last); 16 heads of 64, 450-token prompts 23.1 us.
-// Pages of a part-seen block that no row of the wave sees are left out, scores
-// and values: those chunks 302 us instead of 314 us.
+// did a third block in LDS, raised priority around the products, and sums by dot
+// products of the rounded probabilities.  Measured, 32 query heads on 8 KV heads
+// of 128: chunks of 512 tokens over 8192 keys 302 us (880 TFLOP/s), whole prompts
+// of 4096 620 us (887), chunks of 400 to 512 over 2048 to 8192 keys in any order
+// 192 to 210 us (196 to 233 in the rows' order; 12 us of it the join); 16 heads of
+// 64, 8 prompts of 450 tokens 20.2 us.  Pages of a part-seen block that no row of
+// the wave sees are left out, scores and values: chunks over 8192 keys 302 us
+// instead of 314 us.
 // Head dim 64 with four workgroups a CU instead of three: 230 -> 199 us.
 constexpr int TR = 128;                          // query rows of a tile
 constexpr int KB = 64;                           // keys of a block
