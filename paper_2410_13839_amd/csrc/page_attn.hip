@@ -258,19 +258,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
     const int group = a.n_heads / H, h0 = (hbi - hk * g.hb) * g.gs;      // first head of the block in its group
     const int heads = min(g.gs, group - h0), rows = t.nt * g.gs;
     const int rc = r < rows && r % g.gs < heads ? r : 0;                  // rows that do not exist compute row 0
-    const T* qp = (const T*)a.q + (int64_t)(t.t0 + rc / g.gs) * a.q_stride + (hk * group + h0 + rc % g.gs) * D;
-    uint4 q[sizeof(T) == 2 ? D / 32 : D / 16];
-#pragma unroll
-    for (int j = 0; j < (sizeof(T) == 2 ? D / 32 : D / 16); ++j)
-        q[j] = *reinterpret_cast<const uint4*>(qp + (sizeof(T) == 2 ? 32 * j + 8 * gr : 16 * j + 4 * gr));
-    int rlo, rhi;
-    sight_of(a, g, t, rc, rlo, rhi);
-    // keys that every query of the tile sees: [alo, ahi)
-    int alo, ahi, unused;
-    sight_of(a, g, t, rows - 1, alo, unused);
-    sight_of(a, g, t, 0, unused, ahi);
-    const bool mixed = alo != t.lo || ahi != t.hi;       // some keys of the tile are seen by some of its queries only
-
     const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
     const T* pool = (const T*)a.cache.pool + (size_t)hk * PG * D;
     const int32_t* tab = a.table + (size_t)t.c * a.max_pages;
@@ -288,12 +275,26 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
         pg0 = x >= 0 && x < a.cache.num_pages ? x : -1;
         pg1 = y >= 0 && y < a.cache.num_pages ? y : -1;
     };
+    pages(0);                                                             // (before the queries' loads, as they return in order)
+    const T* qp = (const T*)a.q + (int64_t)(t.t0 + rc / g.gs) * a.q_stride + (hk * group + h0 + rc % g.gs) * D;
+    uint4 q[sizeof(T) == 2 ? D / 32 : D / 16];
+#pragma unroll
+    for (int j = 0; j < (sizeof(T) == 2 ? D / 32 : D / 16); ++j)
+        q[j] = *reinterpret_cast<const uint4*>(qp + (sizeof(T) == 2 ? 32 * j + 8 * gr : 16 * j + 4 * gr));
+    int rlo, rhi;
+    sight_of(a, g, t, rc, rlo, rhi);
+    // keys that every query of the tile sees: [alo, ahi)
+    int alo, ahi, unused;
+    sight_of(a, g, t, rows - 1, alo, unused);
+    sight_of(a, g, t, 0, unused, ahi);
+    const bool mixed = alo != t.lo || ahi != t.hi;       // some keys of the tile are seen by some of its queries only
+
     // (fp32 keys of 128 dimensions: 128 registers a set, one set only)
     constexpr int PD = sizeof(T) * D > 256 ? 1 : 2;
     Keys<T, D> kv[PD];
     int bad[PD] = {};                                                     // bit 0, 1: the pair's page is not there
     auto fetch = [&](Keys<T, D>& x, int& b, int i) {
-        if ((i & 63) == 0) pages(i);
+        if ((i & 63) == 0 && i > 0) pages(i);
         const int x0 = __builtin_amdgcn_readlane(pg0, i & 63), x1 = __builtin_amdgcn_readlane(pg1, i & 63);
         b = (x0 < 0 ? 1 : 0) | (x1 < 0 ? 2 : 0);
         x.load(pool + (size_t)max(x0, 0) * pstr, pool + (size_t)max(x1, 0) * pstr, vofs, r, gr);
@@ -554,6 +555,19 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
     const int r0 = min(32 * wave, rows - 1), r1 = min(32 * wave + 31, rows - 1);
     const int row = min(32 * wave + qc, r1);
     const int hq = row % g.gs < heads ? row % g.gs : 0;   // heads that do not exist compute the block's first
+    const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
+    const bf16_t* pool = (const bf16_t*)a.cache.pool + (size_t)hk * PG * D;
+    const int32_t* tab = a.table + (size_t)t.c * a.max_pages;
+    const int nb = k1 > k0 ? (k1 - k0 + KB - 1) / KB : 0;
+    const int pg_end = min(a.max_pages, (k1 + PG - 1) / PG);
+    // lane i: page i of the next 64 (16 blocks), -1 where there is none
+    auto pages = [&](int blk) {
+        const int p = k0 / PG + 4 * blk + lane;
+        const int x = p < pg_end ? tab[p] : -1;
+        return x >= 0 && x < a.cache.num_pages ? x : -1;
+    };
+    // (before the queries' loads: loads return in order, and the keys' wait for these)
+    int pg_now = pages(0), pg_next = pages(16);
     const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(t.t0 + row / g.gs) * a.q_stride + (hk * group + h0 + hq) * D + 8 * hh;
     // scores are S x c with c > 0: a negative scale turns the queries' signs, scale 0 their values to 0
     const float c = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
@@ -574,18 +588,6 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
     sight_of(a, g, t, rows - 1, tlo, skip);
     const bool mixed = tlo != t.lo || thi != t.hi;       // some keys of the tile are seen by some of its queries only
 
-    const size_t vofs = (size_t)H * PG * D, pstr = 2 * vofs;
-    const bf16_t* pool = (const bf16_t*)a.cache.pool + (size_t)hk * PG * D;
-    const int32_t* tab = a.table + (size_t)t.c * a.max_pages;
-    const int nb = k1 > k0 ? (k1 - k0 + KB - 1) / KB : 0;
-    const int pg_end = min(a.max_pages, (k1 + PG - 1) / PG);
-    // lane i: page i of the next 64 (16 blocks), -1 where there is none
-    auto pages = [&](int blk) {
-        const int p = k0 / PG + 4 * blk + lane;
-        const int x = p < pg_end ? tab[p] : -1;
-        return x >= 0 && x < a.cache.num_pages ? x : -1;
-    };
-    int pg_now = pages(0), pg_next = pages(16);
     // what each lane loads of a page in one step: K's piece of slot `slot`, V's in order
     constexpr int SPP = D / 32;                  // wave steps (1 KB) per page block
     auto stage = [&](int buf, int blk) {
