@@ -947,6 +947,7 @@ int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
 // sums.
 struct AttnCut { AttnGeo g; bool wide; uint64_t acc_bytes, bytes; };
 
+// (of a call with rows and tokens)
 AttnCut attn_cut(const mtp_attention_args& a) {
     AttnCut x{};
     const int group = a.n_heads / a.cache.n_kv_heads;
@@ -1024,7 +1025,7 @@ extern "C" {
 int mtp_pages_attention_workspace_size(const mtp_attention_args* args, uint64_t* bytes) {
     const int rc = mtp::attn_check(args);
     if (rc != MTP_OK || !bytes) return MTP_EINVAL;
-    *bytes = mtp::attn_cut(*args).bytes;
+    *bytes = args->n_rows == 0 || args->n_tokens == 0 ? 0 : mtp::attn_cut(*args).bytes;
     return MTP_OK;
 }
 

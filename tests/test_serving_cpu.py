@@ -285,3 +285,14 @@ def test_a_pool_that_needs_a_gradient_is_refused():
         serving._cache(pool)
     with torch.no_grad():
         assert serving._cache(pool).num_pages == 4
+
+
+@pytest.mark.parametrize("n_rows,n_tokens", [(0, 0), (1, 0), (2, 0), (0, 1), (0, 40)])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_attention_of_nothing_needs_nothing(n_rows, n_tokens, head_dim, dtype):
+    from paper_2410_13839_amd import binding as b
+    a = _attention(_cache(dtype=dtype, head_dim=head_dim), n_rows=n_rows, n_tokens=n_tokens, max_pages=4096)
+    assert b.mtp_pages_attention_workspace_size(a) == 0
+    a.workspace = a.workspace_bytes = 0
+    b.mtp_pages_attention(a, 0)
