@@ -740,3 +740,73 @@ def test_two_graphs_and_eager_calls_in_turn():
             graphs[1].replay()
         torch.cuda.synchronize()
         assert same(outs[0], want[0]) and same(outs[1], want[1]), i
+
+
+def test_calls_of_nothing():
+    s = serving()
+    i = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")
+    for n in (0, 1, 3):                                    # rows without tokens; n == 0: no rows either
+        p = s.plan_pages(i(n), i(n), i(n, 700) - 1, 50, 0)
+        assert host(p.row_start).tolist() == [0] * (n + 1) and host(p.status).tolist() == [0] * 4 and p.slots.shape == (0,)
+        for dtype in (torch.float32, torch.bfloat16):
+            pool = torch.ones((50, 2, 2, 1024), dtype=dtype, device="cuda")
+            q = torch.zeros((0, 4, 64), dtype=dtype, device="cuda")
+            assert s.attend_pages(pool, p.table, p.row_start, p.kv_len, q).shape == (0, 4, 64)
+            s.write_pages(pool, p.slots, q[:, :2], q[:, :2])
+            s.copy_pages(pool, p.copies)
+            assert (pool == 1).all()
+    out = torch.full((5, 4, 64), 7.0, device="cuda")       # no rows: every token keeps what out holds
+    s.attend_pages(torch.ones((50, 2, 2, 1024), device="cuda"), i(0, 9), i(1), i(0), out.clone(), out=out)
+    assert (out == 7.0).all()
+    b = s.select_beams(torch.zeros((0, 3, 9), device="cuda"), torch.zeros((0, 3), device="cuda"), i(0, 3), i(0, 3), 1)
+    assert b.token.shape == (0, 3)
+
+
+def test_beam_select_most_rows():
+    """The largest number of beams, of which a few requests are checked."""
+    R, W, V = 2047, 32, 2049
+    g = torch.Generator(device="cuda").manual_seed(4)
+    lg = torch.randn((R, W, V), generator=g, device="cuda")
+    score = torch.randn((R, W), generator=g, device="cuda")
+    ln = torch.randint(0, 30, (R, W), generator=g, device="cuda").to(torch.int32)
+    dn = (torch.rand((R, W), generator=g, device="cuda") < 0.1).to(torch.int32)
+    got = serving().select_beams(lg, score, ln, dn, 2000, 5, 0.7)
+    for r in (0, 1, 1023, 2046):
+        want = paging.beams(*(host(t[r:r + 1]) for t in (lg, score, ln, dn)), 2000, 5, 0.7)
+        for name, w in zip(("length", "done", "parent", "token"), want[1:]):
+            w = w + r * W if name == "parent" else w
+            assert np.array_equal(host(getattr(got, name))[r:r + 1], w), (r, name)
+        assert (np.abs(host(got.score)[r:r + 1] - want[0]) <= 2.0 ** -21 + 2.0 ** -24 * np.abs(want[0])).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("HQ,H,D", [(2, 2, 64), (6, 2, 128)])
+def test_attention_many_tokens(HQ, H, D, dtype):
+    """Rows of up to 90,000 tokens, a window's keys each; sampled queries against 64 bits.  Errors as in check_attention."""
+    window, kv = 50, np.array([90000, 7, 31013])
+    g = torch.Generator().manual_seed(HQ)
+    pages = int(sum(-(-int(n) // 16) for n in kv))
+    table = tables(np.random.default_rng(1), kv, 5700, pages)
+    pool = torch.randn((pages, 2, H, 16 * D), generator=g).to(dtype)
+    start = np.concatenate([[0], np.cumsum(kv)]).astype(np.int32)
+    q = torch.randn((int(start[-1]), HQ, D), generator=g).to(dtype)
+    out = host(serving().attend_pages(pool.cuda(), dev(table), dev(start), dev(kv), q.cuda(), window=window))
+    bf = dtype == torch.bfloat16
+    pn, qn = pool.float().numpy().astype(np.float64), q.float().numpy().astype(np.float64)
+    for c, pos in ((0, 0), (0, 1), (0, 49), (0, 50), (0, 44444), (0, 89999), (1, 0), (1, 6), (2, 0), (2, 31012)):
+        js = np.arange(max(0, pos - window + 1), pos + 1)
+        pg = table[c, js // 16]
+        k = pn[pg, 0].reshape(len(js), H, 16, D)[np.arange(len(js)), :, js % 16]
+        v = pn[pg, 1].reshape((len(js), H, D, 16) if bf else (len(js), H, 16, D))
+        v = (v.transpose(0, 1, 3, 2) if bf else v)[np.arange(len(js)), :, js % 16]
+        for h in range(HQ):
+            x, kk, vv = qn[start[c] + pos, h], k[:, h // (HQ // H)], v[:, h // (HQ // H)]
+            s = kk @ x / D ** 0.5
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            mag = p @ np.abs(vv)
+            ds = (D + 8) * 2.0 ** -24 * (np.abs(kk) @ np.abs(x)).max() / D ** 0.5 + 2.0 ** -22
+            tol = mag * (2 * ds + 1100 * 2.0 ** -24 + (2.0 ** -8 if bf else 0.0))
+            want = p @ vv
+            tol = tol + np.abs(want) * (2.0 ** -8 if bf else 2.0 ** -24)
+            assert (np.abs(out[start[c] + pos, h] - want) <= tol).all(), (c, pos, h)
