@@ -126,3 +126,60 @@ def test_beam_search_is_refused_out_of_order():
     refused(b.MTP_EINVAL)                                # prompts of two lengths in a request
     b.mtp_beam_advance(s.ctx, s.B, 1)
     s.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_prefill_after_a_search_starts_anew(dtype):
+    """The rows' shared pages, scores and states are gone: the same steps as a session that never searched, and the
+    second search is the first one; two sessions' searches in turn do not meet."""
+    R, W = 2, 4
+    wl, model, s, phons, acs = _setup(dtype, R, W, 2, 256, 0.0)
+    _, _, t, _, _ = _setup(dtype, R, W, 2, 256, 0.0)
+    first = []
+    for _ in range(18):
+        first.append((s.beam_step(W, 0.5), s.logits(1).copy()))
+    s.prefill(phons[::-1], acs[::-1])
+    t.prefill(phons[::-1], acs[::-1])
+    for k in (2, 1, 2, 2, 1):
+        a, b = s.step(k, 2), t.step(k, 2)
+        assert all(np.array_equal(x, y) for x, y in zip(a, b))
+        assert np.array_equal(s.logits(k), t.logits(k))
+    s.prefill(phons, acs)
+    t.prefill(phons, acs)
+    for out, lg in first:
+        for x in (s, t):
+            again = x.beam_step(W, 0.5)
+            assert all(np.array_equal(again[k], out[k]) for k in out)
+            assert np.array_equal(x.logits(1), lg)
+    s.close()
+    t.close()
+
+
+def test_beam_search_after_and_between_other_calls():
+    """Steps before the search, forced tokens in it, and steps of two heads behind it keep every row on its own history."""
+    from paper_2410_13839_amd import binding as b
+    R, W = 2, 3
+    wl, model, s, phons, acs = _setup("f32", R, W, 2, 256, 0.0, max_new=40, eos_min=40)
+    n = R * W
+    hist = [[] for _ in range(n)]
+    for _ in range(3):                                     # alike in every row of a request
+        tok, cnt = s.step(2, 1)
+        for c in range(n):
+            hist[c] += [int(x) for x in tok[c][:cnt[c]]]
+    for i in range(14):
+        out = s.beam_step(W)
+        hist = [list(hist[p]) + [int(out["tokens"][c])] for c, p in enumerate(out["parent"])]
+        if i in (4, 9):                                    # other tokens than the chosen ones
+            forced = np.array([[(7 * i + 3 * c) % 50] for c in range(n)], np.int32)
+            b.mtp_force_tokens(s.ctx, forced, np.ones(n, np.int32))
+            for c in range(n):
+                hist[c][-1] = int(forced[c, 0])
+    tok, cnt = s.step(2, 3)
+    for c in range(n):
+        hist[c] += [int(x) for x in tok[c][:cnt[c]]]
+    s.step(1, 1)
+    lg = s.logits(1)
+    for c in range(n):
+        if EOS_ID not in hist[c]:
+            assert np.abs(oracle_logits_at(model, phons[c], acs[c], hist[c], 1)[0] - lg[c, 0]).max() <= 1e-4, c
+    s.close()
