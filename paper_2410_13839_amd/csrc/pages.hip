@@ -10,7 +10,7 @@
 // the others keep, so that the three steps are one launch.
 // What bounds it: the chain of dependent loads (parent -> lengths -> table ->
 // marks) and the launches, not bytes: 8 rows of 229 pages 6.4 us, 256 beams of
-// 256 pages 14.6 us, 256 rows of 512 15.2 us in three launches.
+// 256 pages 13.5 us, 256 rows of 512 15.2 us in three launches.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -26,7 +26,7 @@ constexpr int ROWS_T = 1024;           // threads of the step that takes every r
 constexpr int PLAN_T = 256;            // threads of the other two
 // One launch up to these sizes: table entries, pages (a byte of LDS each) and
 // rows (a workgroup each, so one or two a CU).  64 rows of 64 pages 7.4 us instead
-// of 11.3 us in three launches, 256 of 256 (beams) 14.6 and 14.8 us, 256 of 512
+// of 11.3 us in three launches, 256 of 256 (beams) 13.5 and 14.8 us, 256 of 512
 // 20.6 and 15.2 us.  Workgroups of 256 threads, whose sums are shorter, for few
 // pieces of 64 entries: 8 rows of 229 pages 6.4 us, 7.8 us with 1024 threads; 256
 // rows of 16 pages 14.7 and 10.2 us.
@@ -113,7 +113,7 @@ __device__ __forceinline__ uint64_t plan_rows(const mtp_plan_args& a, PlanRow (&
         ok = ok && L >= 0 && (int64_t)L + A <= (int64_t)PG * a.max_pages;
         if (ok) {
             r[k] = make_int4(p, L, A, 0);
-            if (a.parent && L % PG) atomicMin(&low[p], c);
+            if (a.parent) atomicMin(&low[p], c);
         }
         bad += ok ? 0 : 1;
     }
@@ -324,31 +324,40 @@ __device__ __forceinline__ int free_byte(const uint4* used, int i, int k) {
 // pages, marks what every row keeps in LDS, a byte a page (stores without
 // atomics: neighbouring pages, which a row mostly has, would queue up at the
 // words of a bitmap).
-template <int NT>
+template <int NT, bool BEAMS>
 __global__ __launch_bounds__(NT) void plan_alone_kernel(mtp_plan_args a) {
     constexpr int FLY = 4;             // pieces in flight per wave
     __shared__ uint4 s_used[ONE_PAGES / 16];
-    __shared__ int2 s_piece[ONE_ENTRIES / 64 + ONE_ROWS];      // up to 64 kept entries of a row: first in table_in, number
+    // up to 64 kept entries of a row: the first in table_in; their number, with BEAMS also bit 7, the last is a partly
+    // filled page, and from bit 8 on how many rows keep the others
+    __shared__ int2 s_piece[ONE_ENTRIES / 64 + ONE_ROWS];
     __shared__ PlanRow s_own;
-    __shared__ int s_low[ONE_ROWS], s_buf[NT / 64], s_before[NT + 1], s_start, s_bad[2];
+    __shared__ int s_low[ONE_ROWS], s_keep[ONE_ROWS], s_buf[NT / 64], s_before[NT + 1], s_start, s_bad[2];
     __shared__ uint64_t s_sum[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = blockIdx.x;
     const bool lead = c == 0;
     const int quads = (a.num_pages + 15) / 16, per = (quads + NT - 1) / NT;
     if (tid < 2) s_bad[tid] = 0;
+    if (BEAMS && tid < ONE_ROWS) s_keep[tid] = 0;
     int bad;
     uint64_t start;
     PlanRow mine[1];
     const uint64_t sum = plan_rows<NT, 1>(a, mine, s_low, s_sum, start, lead, bad);
     if (lead && bad) atomicAdd(&s_bad[0], bad);
     if (tid == c) { s_own = mine[0]; s_start = (int)start; }
-    const int kept = tid < a.n_rows ? row_kept(mine[0]) : 0;
+    // of the rows that continue one parent the lowest keeps all that any of them does and marks it (256 beams of 256 pages
+    // 14.8 us if all of them do)
+    const bool in = tid < a.n_rows && mine[0].y > 0;
+    if (BEAMS && in) atomicAdd(&s_keep[mine[0].x], 1);
+    const int kept = in && (!BEAMS || s_low[mine[0].x] == tid) ? row_kept(mine[0]) : 0;
     int at = (kept + 63) / 64;
     const int pieces = block_scan<NT>(at, s_buf);
     const PlanRow r = s_own;
     const bool fresh = lead || row_need(r) > row_kept(r);      // uniform
     if (fresh) {
-        for (int j = 0; j < kept; j += 64) s_piece[at++] = make_int2(mine[0].x * a.max_pages + j, min(kept - j, 64));
+        const int keepers = BEAMS && kept > 0 ? s_keep[mine[0].x] << 8 : 0, part = BEAMS && kept > mine[0].y / PG ? 128 : 0;
+        for (int j = 0; j < kept; j += 64)
+            s_piece[at++] = make_int2(mine[0].x * a.max_pages + j, min(kept - j, 64) | keepers | (j + 64 >= kept ? part : 0));
         for (int i = tid; i < quads; i += NT) s_used[i] = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
         uint8_t* used = reinterpret_cast<uint8_t*>(s_used);
@@ -360,11 +369,12 @@ __global__ __launch_bounds__(NT) void plan_alone_kernel(mtp_plan_args a) {
                 const int u = u0 + NT / 64 * k;
                 const int2 x = s_piece[min(u, pieces - 1)];
                 n[k] = u < pieces ? x.y : 0;
-                pg[k] = lane < n[k] ? a.table_in[x.x + lane] : -1;
+                pg[k] = lane < (BEAMS ? n[k] & 127 : n[k]) ? a.table_in[x.x + lane] : -1;
             }
 #pragma unroll
             for (int k = 0; k < FLY; ++k) {
                 if ((uint32_t)pg[k] < (uint32_t)a.num_pages) used[pg[k]] = 1;
+                else if (BEAMS) bad += lane >= (n[k] & 127) ? 0 : (n[k] & 128) && lane == (n[k] & 127) - 1 ? 1 : n[k] >> 8;
                 else bad += lane < n[k] ? 1 : 0;
             }
         }
@@ -557,10 +567,13 @@ int mtp_pages_plan(const mtp_plan_args* args, void* hip_stream) {
     hipStream_t st = (hipStream_t)hip_stream;
     const int words = (int)plan_words(a.num_pages);
     if (need == 0) {
-        if (a.n_rows * ((a.max_pages + 63) / 64) <= FEW_PIECES)
-            hipLaunchKernelGGL(plan_alone_kernel<256>, dim3(a.n_rows), dim3(256), 0, st, a);
-        else
-            hipLaunchKernelGGL(plan_alone_kernel<1024>, dim3(a.n_rows), dim3(1024), 0, st, a);
+        if (a.n_rows * ((a.max_pages + 63) / 64) <= FEW_PIECES) {
+            if (a.parent) hipLaunchKernelGGL((plan_alone_kernel<256, true>), dim3(a.n_rows), dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((plan_alone_kernel<256, false>), dim3(a.n_rows), dim3(256), 0, st, a);
+        } else {
+            if (a.parent) hipLaunchKernelGGL((plan_alone_kernel<1024, true>), dim3(a.n_rows), dim3(1024), 0, st, a);
+            else hipLaunchKernelGGL((plan_alone_kernel<1024, false>), dim3(a.n_rows), dim3(1024), 0, st, a);
+        }
         return launched();
     }
     const int cb = (words + ROWS_T * 4 - 1) / (ROWS_T * 4);

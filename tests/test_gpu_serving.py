@@ -104,6 +104,22 @@ def test_plan_reports_what_it_cannot_do():
     assert want["status"][1] >= 3
 
 
+@pytest.mark.parametrize("n,m", [(6, 9), (40, 70), (256, 130), (300, 40)])
+@pytest.mark.parametrize("beams", [False, True])
+def test_plan_counts_bad_entries_of_every_row_that_keeps_them(n, m, beams):
+    rng = np.random.default_rng(n + m)
+    length = rng.integers(0, 16 * m - 20, n)
+    pages = n * m
+    table = tables(rng, length, m, pages)
+    table[rng.random((n, m)) < 0.1] = -1
+    table[rng.random((n, m)) < 0.1] = pages + 3
+    parent = rng.integers(0, n, n) if beams else None
+    add = rng.integers(0, 20, n)
+    add[::7] = -1                                          # (taken as empty: no parent's children)
+    want = check_plan(length, add, table, pages, 12 * n, parent)
+    assert want["status"][2] > 0
+
+
 # ------------------------------------------------------- writes and copies
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,H,D,strided", [(1, 1, 64, False), (5, 3, 64, True), (40, 2, 128, False), (333, 5, 128, True),
