@@ -387,6 +387,17 @@ def test_attention_starts_and_lengths_outside_their_range_are_clamped(dtype):
     assert (np.abs(got - want) <= tol).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,q_len", [([300], [1]), ([300], [200]), ([2000], [33]), ([90, 300, 20], [4, 130, 1]),
+                                      ([40] * 70, [1, 3] * 35)])
+@pytest.mark.parametrize("front", [1, 16, 37, 130])
+def test_attention_tokens_before_the_first_row(front, kv, q_len, dtype):
+    c = attention_case(front, kv, q_len, 4, 2, 64, dtype)
+    c["q"] = torch.cat([torch.full((front, c["q"].shape[1]), NAN, dtype=dtype), c["q"]])
+    c["row_start"], c["T"] = c["row_start"] + front, c["T"] + front
+    check_attention(c)                                     # (the first tokens keep what out holds, as the last do)
+
+
 def test_calls_that_need_a_gradient_are_refused():
     c = attention_case(2, [40], [3], 4, 2, 64, torch.float32)
     q = c["q"][:3].cuda().view(3, 4, 64).requires_grad_()
