@@ -5,19 +5,18 @@
 // A beam's best candidates are its largest logits whatever its normaliser, so
 // one pass over the logits finds both.  One wave takes a chunk of 2048 logits
 // into registers (32 loads in flight a lane), sums their exponentials and
-// keeps the chunk's `beams` best in order: the smallest of (at least `beams`)
-// group maxima bounds the last of them from below, what reaches the bound is
-// gathered into LDS (a few dozen logits) and taken best first.  A request's
-// workgroup then merges the sorted lists of each beam's chunks, and the beams'
-// lists in float64, where a candidate's place is the number of others before it
-// (a binary search in every other beam's list).  With few chunks all of it is
-// one launch.
-// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 12 us
-// for the chunks (2.8 TB/s; 4096 waves load at once and then compute: the
-// exponentials, and eight rounds of places) and 8 us for the merge, a chain of
-// loads, a float64 exponential, logarithm and power, and eight rounds of a wave
-// maximum per beam.  One request of 4 beams over 1025 logits 8 us: the launch and
-// the same chain.
+// keeps the chunk's `beams` best in order: maxima of lanes or groups of them
+// bound the last of those from below, what reaches the bound is gathered into LDS
+// (a few dozen logits) and taken best first.  A request's workgroup then merges
+// the sorted lists of each beam's chunks, and the beams' lists in float64.  With
+// few chunks all of it is one launch.
+// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 10.2 us
+// for the chunks (3.3 TB/s; 4096 waves load at once and then compute) and 8 us
+// for the merge, a chain of loads, a float64 exponential, logarithm and power, and
+// eight rounds of a wave maximum per beam.  More than 256 list entries of a beam
+// are merged head by head, a lane a chunk (1 request of 8 beams over 131,072
+// logits 15.3 us; 28.8 us with all entries compared every round).  One request of
+// 4 beams over 1025 logits 8 us: the launch and the same chain.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -33,6 +32,15 @@ constexpr int MAX_BEAMS = 32;
 constexpr int NV = 32;                   // logits per lane
 constexpr int CHUNK = 64 * NV;           // logits per wave
 constexpr int CAP = 256;                 // gathered candidates per wave
+// Up to this many beams a chunk's bound comes from groups of lanes (4 beams over
+// 32,000 logits 12.7 us either way; 5 beams 19.0 us with groups and 17.0 us with
+// the lanes' maxima, 16 over 50,000 37 and 31 us).
+constexpr int FEW_BEAMS = 4;
+// Up to this many beams the next ones are found by counting places, a thread per
+// candidate and other beam (8 beams over 65,536 logits 20.7 us, 21.5 us head by
+// head; 16 over 2000 18.0 and 16.9 us, 32 over 32,000 127 and 56 us).
+constexpr int PLACED = 12;
+constexpr int HELD = 1024;               // list entries of a beam that a merging wave takes into LDS
 constexpr int FUSED_UNITS = 32;          // chunks per request up to which one launch does everything
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -90,13 +98,21 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
         f[i] = fmaxf(f[i], -INFINITY);           // NaN: -infinity
         top = fmaxf(top, f[i]);
     }
-    // maxima of groups of lanes, at least W groups; bound: the smallest of them
-    float grp = top;
-    if (W <= 32) grp = fmaxf(grp, dpp_f<DPP_XOR1>(grp));
-    if (W <= 16) grp = fmaxf(grp, dpp_f<DPP_XOR2>(grp));
-    if (W <= 8) grp = fmaxf(grp, dpp_f<DPP_HALF_MIRROR>(grp));
-    if (W <= 4) grp = fmaxf(grp, dpp_f<DPP_ROR8>(grp));
-    float bound = grp;
+    // a bound that at least W of the chunk's logits reach: the W-th largest of the lanes' maxima, or (fewer instructions,
+    // more logits that reach it) the smallest maximum of at least W groups of lanes
+    float bound;
+    if (W > FEW_BEAMS) {
+        int above = 0;
+#pragma unroll
+        for (int k = 0; k < 64; ++k) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(top), k)) > top ? 1 : 0;
+        bound = above < W ? top : INFINITY;
+        bound = min_f(bound, dpp_f<DPP_XOR1>(bound));
+    } else {
+        bound = fmaxf(top, dpp_f<DPP_XOR1>(top));
+        bound = fmaxf(bound, dpp_f<DPP_XOR2>(bound));
+        bound = fmaxf(bound, dpp_f<DPP_HALF_MIRROR>(bound));
+        if (W <= 4) bound = fmaxf(bound, dpp_f<DPP_ROR8>(bound));
+    }
     bound = min_f(bound, dpp_f<DPP_XOR2>(bound));
     bound = min_f(bound, dpp_f<DPP_HALF_MIRROR>(bound));
     bound = min_f(bound, dpp_f<DPP_ROR8>(bound));
@@ -216,8 +232,31 @@ struct BeamLds {
     int len[MAX_BEAMS], done[MAX_BEAMS];
     float2 best[MAX_BEAMS][MAX_BEAMS];           // each beam's best logits over its chunks
     double rank[MAX_BEAMS][MAX_BEAMS];           // its candidates, best first
-    int place[MAX_BEAMS * MAX_BEAMS];            // each candidate's place among all
+    int place[PLACED * PLACED];                  // each candidate's place among all
+    int win[MAX_BEAMS];                          // the chosen: beam * MAX_BEAMS + place in its list
 };
+
+// The id of the largest value among lanes 0 .. W - 1 (W <= 32), of equal
+// ones the lowest; uniform.
+__device__ __forceinline__ int best_head(double v, int id, int W) {
+    auto take = [&](double ov, int oi) {
+        const bool better = (int)(ov > v) | ((int)(ov == v) & (int)(oi < id));
+        v = better ? ov : v;
+        id = better ? oi : id;
+    };
+    auto join = [](int lo, int hi) { return __longlong_as_double((long long)(uint32_t)lo | (long long)hi << 32); };
+#define STEP(CTRL) take(join(dpp_i<CTRL>(__double2loint(v)), dpp_i<CTRL>(__double2hiint(v))), dpp_i<CTRL>(id))
+    STEP(DPP_XOR1);
+    STEP(DPP_XOR2);
+    STEP(DPP_HALF_MIRROR);
+    if (W > 8) STEP(DPP_ROR8);
+#undef STEP
+    if (W > 16) {
+        const double ov = join(__builtin_amdgcn_readlane(__double2loint(v), 16), __builtin_amdgcn_readlane(__double2hiint(v), 16));
+        take(ov, __builtin_amdgcn_readlane(id, 16));
+    }
+    return __builtin_amdgcn_readfirstlane(id);
+}
 
 // The request's state, by the workgroup's last wave (read after a barrier).
 template <int NW>
@@ -234,7 +273,7 @@ __device__ __forceinline__ void beam_state(const mtp_beam_args& a, int r, BeamLd
 // entries a beam.
 template <int NW, bool FEW>
 __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const float* max, const double* sum,
-                                           const float2* list, int chunks, BeamLds& s) {
+                                           const float2* list, int chunks, BeamLds& s, float2* held) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.beams, n = min(W, a.vocab);
     for (int b = wave; b < W; b += NW) {
         if (a.done[r * W + b] > 0) continue;     // uniform over the wave
@@ -259,10 +298,24 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
             few.best(n, s.best[b]);
             continue;
         }
-        if (entries <= 64 * NV) {
-            BeamList<NV> many;
-            many.load(bl, entries);
-            many.best(n, s.best[b]);
+        const float2* src = bl;
+        if (entries <= HELD) {
+            for (int i = lane; i < entries; i += 64) held[i] = bl[i];
+            __builtin_amdgcn_wave_barrier();
+            src = held;
+        }
+        if (chunks <= 64) {
+            // lane i: the head of chunk i's list
+            const float2 none = make_float2(-INFINITY, __int_as_float(0x7fffffff));
+            int pos = 0;
+            float2 head = lane < chunks ? src[lane * W] : none;
+            for (int w = 0; w < n; ++w) {
+                float bv = head.x;
+                int bi = __float_as_int(head.y);
+                wave_argmax_uniform(bv, bi);
+                if (lane == 0) s.best[b][w] = make_float2(bv, __int_as_float(bi));
+                if (__float_as_int(head.y) == bi) head = ++pos < W ? src[lane * W + pos] : none;
+            }
             continue;
         }
         // lane i: the heads of the lists of chunks i, i + 64, ... (the best of them, advanced past what was taken)
@@ -276,7 +329,7 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
                 hv = -INFINITY; hi = 0x7fffffff;
                 for (int i = lane; i < chunks; i += 64)
                     for (int k = 0; k < W; ++k) {
-                        const float2 e = bl[(size_t)i * W + k];
+                        const float2 e = src[(size_t)i * W + k];
                         const int id = __float_as_int(e.y);
                         if (before(pv, pi, e.x, id)) {
                             if (before(e.x, id, hv, hi)) { hv = e.x; hi = id; }
@@ -312,26 +365,44 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
         const int b = c / n, j = c - b * n;
         int tok;
         s.rank[b][j] = candidate(b, j, tok) / s.den[b];
-        s.place[c] = j;                          // those of its own beam before it
+        if (W <= PLACED) s.place[c] = j;
     }
     __syncthreads();
-    // a candidate's place: how many of every other beam's come before it (equal ones: those of the earlier beam)
-    for (int p = threadIdx.x; p < W * n * W; p += 64 * NW) {
-        const int c = p / W, o = p - c * W, b = c / n, j = c - b * n;
-        if (o == b) continue;
-        const double mine = s.rank[b][j];
-        int lo = 0, hi = n;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            const double r2 = s.rank[o][mid];
-            if (r2 > mine || (r2 == mine && o < b)) lo = mid + 1; else hi = mid;
+    if (W > PLACED) {
+        // the best of the lists' heads, W times; equal ones: the earlier beam's
+        if (wave == 0) {
+            int pos = 0, id = lane < W ? lane : 64 + lane;
+            double head = lane < W ? s.rank[lane][0] : -INFINITY;
+            for (int w = 0; w < W; ++w) {
+                const int best = best_head(head, id, W);
+                if (id != best) continue;
+                s.win[w] = lane * MAX_BEAMS + pos++;
+                head = pos < n ? s.rank[lane][pos] : -INFINITY;
+                id = pos < n ? lane : 64 + lane;
+            }
         }
-        if (lo) atomicAdd(&s.place[c], lo);
+    } else {
+        // a candidate's place: those of its own beam before it, and how many of every other beam's come before it
+        // (equal ones: those of the earlier beam)
+        for (int p = threadIdx.x; p < W * n * W; p += 64 * NW) {
+            const int c = p / W, o = p - c * W, b = c / n, j = c - b * n;
+            if (o == b) continue;
+            const double mine = s.rank[b][j];
+            int lo = 0, hi = n;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                const double r2 = s.rank[o][mid];
+                if (r2 > mine || (r2 == mine && o < b)) lo = mid + 1; else hi = mid;
+            }
+            if (lo) atomicAdd(&s.place[c], lo);
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < W * n; c += 64 * NW)
+            if (s.place[c] < W) s.win[s.place[c]] = c / n * MAX_BEAMS + c % n;
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < W * n; c += 64 * NW) {
-        if (s.place[c] >= W) continue;
-        const int b = c / n, j = c - b * n, o = r * W + s.place[c];
+    for (int w = threadIdx.x; w < W; w += 64 * NW) {
+        const int b = s.win[w] / MAX_BEAMS, j = s.win[w] % MAX_BEAMS, o = r * W + w;
         int tok;
         const double total = candidate(b, j, tok);
         a.out_score[o] = (float)total;
@@ -358,7 +429,7 @@ __global__ __launch_bounds__(64 * NW) void beam_fused_kernel(mtp_beam_args a) {
         beam_chunk(a, r * W + b, u - b * chunks, s_list + u * W, &s_max[u], &s_sum[u], s_buf[wave]);
     }
     __syncthreads();
-    beam_merge<NW, true>(a, r, s_max, s_sum, s_list, chunks, s);
+    beam_merge<NW, true>(a, r, s_max, s_sum, s_list, chunks, s, nullptr);
 }
 
 __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs w, int chunks) {
@@ -372,9 +443,10 @@ __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs
 template <int NW, bool FEW>
 __global__ __launch_bounds__(64 * NW) void beam_merge_kernel(mtp_beam_args a, BeamWs w, int chunks) {
     __shared__ BeamLds s;
+    __shared__ float2 s_held[FEW ? 1 : NW][FEW ? 1 : HELD];
     const size_t u = (size_t)blockIdx.x * a.beams * chunks;
     beam_state<NW>(a, blockIdx.x, s);
-    beam_merge<NW, FEW>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s);
+    beam_merge<NW, FEW>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s, s_held[FEW ? 0 : threadIdx.x >> 6]);
 }
 
 // ------------------------------------------------- a context's beams
@@ -481,7 +553,7 @@ int mtp_beam_select(const mtp_beam_args* args, void* hip_stream) {
         if (a.beams * chunks <= 256)
             hipLaunchKernelGGL((beam_merge_kernel<16, true>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
         else
-            hipLaunchKernelGGL((beam_merge_kernel<8, false>), dim3(a.n_requests), dim3(512), 0, st, a, w, chunks);
+            hipLaunchKernelGGL((beam_merge_kernel<16, false>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
     }
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
