@@ -10,12 +10,12 @@
 // (a few dozen logits) and taken best first.  A request's workgroup then merges
 // the sorted lists of each beam's chunks, and the beams' lists in float64.  With
 // few chunks all of it is one launch.
-// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 10.2 us
-// for the chunks (3.3 TB/s; 4096 waves load at once and then compute) and 8 us
+// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 10.4 us
+// for the chunks (3.2 TB/s; 4096 waves load at once and then compute) and 7.7 us
 // for the merge, a chain of loads, a float64 exponential, logarithm and power, and
-// eight rounds of a wave maximum per beam.  More than 256 list entries of a beam
-// are merged head by head, a lane a chunk (1 request of 8 beams over 131,072
-// logits 15.3 us; 28.8 us with all entries compared every round).  One request of
+// eight rounds of a wave maximum per beam.  A beam's lists are merged head by
+// head, a lane a chunk (1 request of 8 beams over 131,072 logits 14.9 us; 28.8 us
+// with all entries compared every round).  One request of
 // 4 beams over 1025 logits 8 us: the launch and the same chain.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -40,7 +40,6 @@ constexpr int FEW_BEAMS = 4;
 // candidate and other beam (8 beams over 65,536 logits 20.7 us, 21.5 us head by
 // head; 16 over 2000 18.0 and 16.9 us, 32 over 32,000 127 and 56 us).
 constexpr int PLACED = 12;
-constexpr int HELD = 1024;               // list entries of a beam that a merging wave takes into LDS
 // Chunks per request up to which one launch does everything, a wave each (8
 // requests of 4 beams over 16,384 logits, 32 chunks: 18.5 us, 12.9 us in two
 // launches; 64 of 8 over 1025, 8 chunks: 10.3 and 11.4 us).
@@ -197,37 +196,6 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
     }
 }
 
-// One wave's (logit, index bits) pairs, at most 64 N, and the n best of them.
-template <int N>
-struct BeamList {
-    float f[N];
-    int id[N];
-    __device__ __forceinline__ void load(const float2* list, int entries) {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const bool in = 64 * i + lane < entries;
-            const float2 e = list[in ? 64 * i + lane : 0];
-            f[i] = in ? e.x : -INFINITY;
-            id[i] = in ? __float_as_int(e.y) : 0x7fffffff;
-        }
-    }
-    __device__ __forceinline__ void best(int n, float2* out) const {
-        float pv = INFINITY;
-        int pi = -1;
-        for (int w = 0; w < n; ++w) {
-            float bv = -INFINITY;
-            int bi = 0x7fffffff;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (before(pv, pi, f[i], id[i]) & before(f[i], id[i], bv, bi)) { bv = f[i]; bi = id[i]; }
-            wave_argmax_uniform(bv, bi);
-            if ((threadIdx.x & 63) == 0) out[w] = make_float2(bv, __int_as_float(bi));
-            pv = bv; pi = bi;
-        }
-    }
-};
-
 // The waves' own scratch.
 struct BeamLds {
     double lse[MAX_BEAMS], den[MAX_BEAMS];
@@ -272,9 +240,10 @@ __device__ __forceinline__ void beam_state(const mtp_beam_args& a, int r, BeamLd
 }
 
 // A request's merge by a workgroup of NW waves.  max, sum, list: the request's
-// own, [beams][chunks] and [beams][chunks][beams].  FEW: at most 256 list
-// entries a beam.
-template <int NW, bool FEW>
+// own, [beams][chunks] and [beams][chunks][beams].  held: room for HOLD entries of
+// this wave's, into which it takes a beam's lists that fit; HOLD 0: they are in
+// LDS already.
+template <int NW, int HOLD>
 __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const float* max, const double* sum,
                                            const float2* list, int chunks, BeamLds& s, float2* held) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.beams, n = min(W, a.vocab);
@@ -282,8 +251,13 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
         if (a.done[r * W + b] > 0) continue;     // uniform over the wave
         const float2* bl = list + (size_t)b * chunks * W;
         const int entries = chunks * W;
-        BeamList<4> few;                         // (its loads in flight during the sums below)
-        if (chunks > 1 && (FEW || entries <= 64 * 4)) few.load(bl, entries);
+        const bool holds = HOLD > 0 && entries <= HOLD;
+        constexpr int PRE = HOLD <= 256 ? HOLD / 64 : 0;      // of a lane in flight during the sums below (more would spill)
+        float2 pre[PRE + 1];
+        if (holds) {
+#pragma unroll
+            for (int i = 0; i < PRE; ++i) pre[i] = bl[min(64 * i + lane, entries - 1)];
+        }
         const float* bm = max + (size_t)b * chunks;
         const double* bs = sum + (size_t)b * chunks;
         float m = -INFINITY;
@@ -297,13 +271,13 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
             if (lane < n) s.best[b][lane] = bl[lane];
             continue;
         }
-        if (FEW || entries <= 64 * 4) {
-            few.best(n, s.best[b]);
-            continue;
-        }
         const float2* src = bl;
-        if (entries <= HELD) {
-            for (int i = lane; i < entries; i += 64) held[i] = bl[i];
+        if (holds) {
+            __builtin_amdgcn_wave_barrier();     // (the last beam's are read)
+#pragma unroll
+            for (int i = 0; i < PRE; ++i)
+                if (64 * i + lane < entries) held[64 * i + lane] = pre[i];
+            for (int i = 64 * PRE + lane; i < entries; i += 64) held[i] = bl[i];
             __builtin_amdgcn_wave_barrier();
             src = held;
         }
@@ -432,7 +406,7 @@ __global__ __launch_bounds__(64 * NW) void beam_fused_kernel(mtp_beam_args a) {
         beam_chunk(a, r * W + b, u - b * chunks, s_list + u * W, &s_max[u], &s_sum[u], s_buf[wave]);
     }
     __syncthreads();
-    beam_merge<NW, true>(a, r, s_max, s_sum, s_list, chunks, s, nullptr);
+    beam_merge<NW, 0>(a, r, s_max, s_sum, s_list, chunks, s, nullptr);
 }
 
 __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs w, int chunks) {
@@ -443,13 +417,13 @@ __global__ __launch_bounds__(256) void beam_chunk_kernel(mtp_beam_args a, BeamWs
     beam_chunk(a, row, ch, w.list + u * a.beams, &w.max[u], &w.sum[u], s_buf[wave]);
 }
 
-template <int NW, bool FEW>
+template <int NW, int HOLD>
 __global__ __launch_bounds__(64 * NW) void beam_merge_kernel(mtp_beam_args a, BeamWs w, int chunks) {
     __shared__ BeamLds s;
-    __shared__ float2 s_held[FEW ? 1 : NW][FEW ? 1 : HELD];
+    __shared__ float2 s_held[NW][HOLD];
     const size_t u = (size_t)blockIdx.x * a.beams * chunks;
     beam_state<NW>(a, blockIdx.x, s);
-    beam_merge<NW, FEW>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s, s_held[FEW ? 0 : threadIdx.x >> 6]);
+    beam_merge<NW, HOLD>(a, blockIdx.x, w.max + u, w.sum + u, w.list + u * a.beams, chunks, s, s_held[threadIdx.x >> 6]);
 }
 
 // ------------------------------------------------- a context's beams
@@ -554,9 +528,9 @@ int mtp_beam_select(const mtp_beam_args* args, void* hip_stream) {
     } else {
         hipLaunchKernelGGL(beam_chunk_kernel, dim3((chunks + 3) / 4, a.n_requests * a.beams), dim3(256), 0, st, a, w, chunks);
         if (a.beams * chunks <= 256)
-            hipLaunchKernelGGL((beam_merge_kernel<16, true>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
+            hipLaunchKernelGGL((beam_merge_kernel<16, 256>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
         else
-            hipLaunchKernelGGL((beam_merge_kernel<16, false>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
+            hipLaunchKernelGGL((beam_merge_kernel<16, 1024>), dim3(a.n_requests), dim3(1024), 0, st, a, w, chunks);
     }
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }
