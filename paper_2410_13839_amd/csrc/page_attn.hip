@@ -106,7 +106,9 @@ __device__ __forceinline__ AttnTile find_item(const mtp_attention_args& a, const
     const int lane = threadIdx.x & 63, c = min(lane, a.n_rows - 1);
     const int s = start_of(a, c), e = start_of(a, c + 1), kv = keys_of(a, c);
     const int count = lane < a.n_rows && e > s ? (e - s + g.tt - 1) / g.tt : 0;
-    const int whole = min(kv / g.split_len, g.n_splits), rest = whole < g.n_splits ? kv - whole * g.split_len : -1;
+    // what a tile sees of them (in a window from a multiple of 32 on, as runs_of cuts it)
+    const int see = a.window > 0 ? min(kv, min(a.window, 1 << 21) + g.tt + 31) : kv;
+    const int whole = min(see / g.split_len, g.n_splits), rest = whole < g.n_splits ? see - whole * g.split_len : -1;
     const int c0 = count * whole, c1 = rest >= 0 ? count : 0;
     int b0 = 0, b1 = 0, all0 = 0;                // items before this lane's whole runs and before its rest
     for (int k = 0; k < a.n_rows; ++k) {
@@ -953,7 +955,6 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     const int group = a.n_heads / a.cache.n_kv_heads;
     x.g.hb = (group + 15) / 16;
     x.g.gs = (group + x.g.hb - 1) / x.g.hb;
-    const int64_t kv_all = (int64_t)PG * a.max_pages, kv = a.max_kv > 0 && a.max_kv < kv_all ? a.max_kv : kv_all;
     // The wide kernel from this many query rows a cache row on (16 rows, 8 KV heads, 1000 to 4000 keys: head dim 128, 8
     // rows 54.5 us wide and 57.8 us narrow, 4 rows of 32 sequences 309 and 224 us; head dim 64, 64 rows 55 and 57 us,
     // 48 rows 57 and 46 us).
@@ -963,6 +964,11 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     x.g.tt = rt / x.g.gs;
     x.g.n_tiles = a.n_rows == 1 ? (a.n_tokens + x.g.tt - 1) / x.g.tt : a.n_tokens / x.g.tt + a.n_rows;
     const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
+    // the most keys that a tile sees, as far as the host knows (32 single tokens of up to 16,384 keys in a window of 1024:
+    // 26 us, 36 us cut as if they saw all)
+    int64_t kv = (int64_t)PG * a.max_pages;
+    if (a.max_kv > 0) kv = std::min<int64_t>(kv, a.max_kv);
+    if (a.window > 0) kv = std::min<int64_t>(kv, (int64_t)a.window + x.g.tt + 31);
     // Sorting costs a workgroup some 25 ns a row, more than it gives few query rows on short keys (40 single tokens over
     // up to 700 keys, 16 heads: 19.1 us in the tiles' order, 20.1 us sorted; 32 over up to 1190 keys 27.8 and 27.0 us;
     // wide, 16 rows of 300 to 750 tokens over up to 150: 21.4 and 20.5 us).
