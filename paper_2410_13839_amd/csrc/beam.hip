@@ -76,8 +76,8 @@ __device__ __forceinline__ int before(float va, int ia, float vb, int ib) {
 __device__ __forceinline__ float min_f(float a, float b) { return a < b ? a : b; }
 
 // One wave: chunk `ch` of row `row`; list[0 .. beams) gets its best logits
-// (-infinity and indexes past the vocabulary behind the chunk's end), mx and
-// sum its normaliser's part.  buf: CAP entries of LDS of this wave.
+// (-infinity and the last index behind what the chunk has), mx and sum its
+// normaliser's part.  buf: CAP entries of LDS of this wave.
 __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int ch, float2* list, float* mx_out,
                                            double* sum_out, float2* buf) {
     const int lane = threadIdx.x & 63, W = a.beams;
@@ -113,7 +113,7 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
         bound = fmaxf(top, dpp_f<DPP_XOR1>(top));
         bound = fmaxf(bound, dpp_f<DPP_XOR2>(bound));
         bound = fmaxf(bound, dpp_f<DPP_HALF_MIRROR>(bound));
-        if (W <= 4) bound = fmaxf(bound, dpp_f<DPP_ROR8>(bound));
+        bound = fmaxf(bound, dpp_f<DPP_ROR8>(bound));
     }
     bound = min_f(bound, dpp_f<DPP_XOR2>(bound));
     bound = min_f(bound, dpp_f<DPP_HALF_MIRROR>(bound));
@@ -136,6 +136,12 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     if (lane == 0) { *mx_out = m; *sum_out = sum; }
 
+    if (__any(bound == -INFINITY)) {
+        // nothing behind the vocabulary reaches it (4 requests of 11 beams over 2057 logits 16.4 us, 30.7 us with all of
+        // the last chunk gathered)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) f[i] = v0 + 64 * i < a.vocab ? f[i] : NAN;
+    }
     int n = 0;                                   // uniform
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -157,6 +163,7 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
             place += before(v, __builtin_amdgcn_readlane(id, k), e.x, id);
         }
         if (lane < n && place < W) list[place] = e;
+        if (lane >= n && lane < W) list[lane] = make_float2(-INFINITY, __int_as_float(0x7fffffff));
         return;
     }
     float pv = INFINITY;                         // the last one taken
