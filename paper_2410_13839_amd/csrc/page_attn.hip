@@ -955,20 +955,28 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     const int group = a.n_heads / a.cache.n_kv_heads;
     x.g.hb = (group + 15) / 16;
     x.g.gs = (group + x.g.hb - 1) / x.g.hb;
-    // The wide kernel from this many query rows a cache row on (16 rows, 8 KV heads, 1000 to 4000 keys: head dim 128, 8
-    // rows 54.5 us wide and 57.8 us narrow, 4 rows of 32 sequences 309 and 224 us; head dim 64, 64 rows 55 and 57 us,
-    // 48 rows 57 and 46 us).
+    // the most keys that a query sees, as far as the host knows
+    int64_t kv = (int64_t)PG * a.max_pages;
+    if (a.max_kv > 0) kv = std::min<int64_t>(kv, a.max_kv);
+    if (a.window > 0) kv = std::min<int64_t>(kv, a.window);
+    // The wide kernel from this many query rows a cache row on (16 rows, 8 KV heads, 1000 to 4000 keys from HBM: head dim
+    // 128, 8 rows 41.5 us wide and 58.9 us narrow; head dim 64, 64 rows 55 and 57 us, 48 rows 57 and 46 us), where the
+    // work is past its latency.  That is counted in pairs of a 16-row tile and a key: 250,000 with head dim 128 (one
+    // sequence of 32 tokens over 4000 keys, 32 heads on 8, 256,000 pairs: 17.6 us wide and 20.1 us narrow; of 8 tokens
+    // over 1000 keys, 8 heads on 2, 4000 pairs: 18 and 11 us), 500,000 with 64 (4 sequences of 32 tokens, 32 heads on 8:
+    // 1000 keys, 256,000 pairs, 18 and 11 us; 4000 keys, a million, 25 us either way).
     const bool d128 = a.cache.head_dim == 128;
-    x.wide = a.cache.dtype == MTP_DTYPE_BF16 && (int64_t)a.n_tokens * x.g.gs >= (d128 ? 8ll : 64ll) * a.n_rows;
+    const int64_t query_rows = (int64_t)a.n_tokens * x.g.gs;
+    const int64_t pairs = std::max<int64_t>(a.n_rows, query_rows / 16) * a.cache.n_kv_heads * x.g.hb * kv;
+    x.wide = a.cache.dtype == MTP_DTYPE_BF16 && query_rows >= (d128 ? 8ll : 64ll) * a.n_rows &&
+             pairs >= (d128 ? 250000ll : 500000ll);
     const int rt = x.wide ? TR : 16;
     x.g.tt = rt / x.g.gs;
     x.g.n_tiles = a.n_rows == 1 ? (a.n_tokens + x.g.tt - 1) / x.g.tt : a.n_tokens / x.g.tt + a.n_rows;
     const int64_t work = (int64_t)x.g.n_tiles * a.cache.n_kv_heads * x.g.hb;
-    // the most keys that a tile sees, as far as the host knows (32 single tokens of up to 16,384 keys in a window of 1024:
-    // 26 us, 36 us cut as if they saw all)
-    int64_t kv = (int64_t)PG * a.max_pages;
-    if (a.max_kv > 0) kv = std::min<int64_t>(kv, a.max_kv);
-    if (a.window > 0) kv = std::min<int64_t>(kv, (int64_t)a.window + x.g.tt + 31);
+    // the most that a tile sees (32 single tokens of up to 16,384 keys in a window of 1024: 26 us, 36 us cut as if they
+    // saw all)
+    if (a.window > 0) kv = std::min<int64_t>(kv + x.g.tt + 31, (int64_t)PG * a.max_pages);
     // Sorting costs a workgroup some 25 ns a row, more than it gives few query rows on short keys (40 single tokens over
     // up to 700 keys, 16 heads: 19.1 us in the tiles' order, 20.1 us sorted; 32 over up to 1190 keys 27.8 and 27.0 us;
     // wide, 16 rows of 300 to 750 tokens over up to 150: 21.4 and 20.5 us).
@@ -980,7 +988,8 @@ AttnCut attn_cut(const mtp_attention_args& a) {
     // 8192 keys: two runs 93 us, three 79; 3 rows of 64 to 600 over up to 6000: four 51 us, five 60).  No run shorter
     // than 256 keys.  Narrow: 512 workgroups, runs of 128 keys at least, at most 32 of them (16,000 keys of 8 KV heads 26
     // us, 33 us in 64); whole below 512 keys (400 keys of 16 heads 7.4 us, 8.1 us in three runs) and where the tiles fill
-    // three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us, 38 us in three).  But runs of 1024 keys of
+    // three quarters of the CUs (8 rows of up to 3650 keys, 240 tiles, 34.5 us, 38 us in three) or, below 2048 keys, a
+    // third (16 rows of 16 tokens over 1000 keys, 8 heads of 64 on 2, 160 tiles, 11 us, 15 us in four).  But runs of 1024 keys of
     // long caches, which even out ragged rows, while the tiles are part full, up to ten workgroups a CU (8 rows of 32
     // tokens over 3000 to 8000 keys, 8 heads of 64: 54 us whole, 34 us in seven; 32 single tokens over up to 16,384: 242
     // us in two, 210 in eight, 225 in twelve).
@@ -992,7 +1001,7 @@ AttnCut attn_cut(const mtp_attention_args& a) {
         if (!few && !d128) n = std::max<int64_t>(n, std::min<int64_t>(runs(1152), 4));
         n = std::min<int64_t>(n, kv / 256);
     } else {
-        n = kv < 512 || work >= 192 ? 1 : std::min<int64_t>(std::min<int64_t>(runs(512), kv / 128), 32);
+        n = kv < 512 || work >= (kv < 2048 ? 96 : 192) ? 1 : std::min<int64_t>(std::min<int64_t>(runs(512), kv / 128), 32);
         if (kv >= 4096 && few) n = std::max<int64_t>(n, std::min<int64_t>(kv / 1024, 2560 / work));
     }
     n = std::max<int64_t>(1, std::min<int64_t>(n, MAX_RUNS));

@@ -171,13 +171,16 @@ def test_copy(shape, dtype):
 
 
 # --------------------------------------------------------------- attention
+WIDTH = 0                                                  # of every case's table, where it is more than the rows need
+
+
 def attention_case(seed, kv, q_len, HQ, H, D, dtype, strided=False, spare=3, nan_behind=True):
     g = torch.Generator().manual_seed(seed)
     rng = np.random.default_rng(seed)
     kv, q_len = np.asarray(kv), np.asarray(q_len)
     m = max(1, int(-(-kv.max() // 16))) + seed % 3
     pages = int(sum(-(-int(n) // 16) for n in kv)) + spare
-    table = tables(rng, kv, m, pages)
+    table = tables(rng, kv, max(m, WIDTH), pages)
     pool = torch.randn((pages, 2, H, 16 * D), generator=g).to(dtype)
     if nan_behind:                               # what lies behind a row's last key must not matter
         kp = pool[:, 0].view(pages, H, 16, D)
@@ -385,6 +388,45 @@ def test_attention_starts_and_lengths_outside_their_range_are_clamped(dtype):
                                       q.cuda().view(77, 4, 64)).float())
     tol = bound[0] * (2.0 ** -8 if bf else 0.0) + np.abs(want) * (2.0 ** -8 if bf else 0.0) + 1e-4 * bound[0] + 1e-30
     assert (np.abs(got - want) <= tol).all()
+
+
+@pytest.fixture(params=[1100, 4096, 65536])
+def wide_tables(request):
+    """The same cases in tables for longer rows, which the calls are cut for: other tiles and runs of the keys."""
+    global WIDTH
+    WIDTH = request.param
+    yield
+    WIDTH = 0
+
+
+@pytest.mark.parametrize("HQ,H,D", [(2, 2, 64), (8, 2, 128), (7, 1, 64), (3, 3, 128), (20, 1, 128), (16, 8, 64), (8, 8, 128)])
+def test_attention_in_wide_tables(wide_tables, HQ, H, D):
+    for i in range(len(LENGTHS)):
+        test_attention_causal(i, HQ, H, D, torch.bfloat16)
+    for kv, q_len in (([50, 0, 129], [3, 9, 140]), ([1], [70]), ([700, 16], [1, 1]), ([90, 33, 64], [64, 65, 1])):
+        test_attention_full(kv, q_len, HQ, H, D, torch.bfloat16)
+    for w in (1, 37, 200, 100000):
+        check_attention(attention_case(w, [400, 63, 700], [130, 1, 3], HQ, H, D, torch.bfloat16), window=w)
+
+
+def test_attention_edges_in_wide_tables(wide_tables):
+    bf = torch.bfloat16
+    for q in (1, 4, 150):
+        test_attention_rows_that_see_nothing(q, bf)
+        test_attention_pages_outside_the_pool_are_not_seen(q, bf)
+    for HQ, H, D, q in ((2, 2, 64, 4), (4, 1, 128, 4), (2, 2, 64, 150), (4, 2, 128, 200)):
+        test_attention_what_is_not_seen_never_matters(HQ, H, D, q, bf)
+    for scale in (0.0, -0.3, 2.0):
+        test_attention_scales(scale, bf)
+    test_attention_large_scores(bf)
+    for D in (64, 128):
+        for kv, q in ((60, 1), (3000, 1), (900, 130), (3000, 130)):
+            test_attention_infinite_values_of_no_weight_show(D, kv, q, 0, bf)
+
+
+@pytest.mark.parametrize("D,window", [(128, 300), (64, 450), (128, 1000)])
+def test_attention_window_of_long_chunks(D, window):
+    check_attention(attention_case(D, [1300, 0, 707], [600, 3, 600], 16, 8, D, torch.bfloat16), window=window)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
