@@ -131,7 +131,7 @@ struct WsLayout {
     uint64_t rows, ids, tiles, last_row, state, btab, h, q, qh, u, attn, ffn, part, apart, kvnew, fsync, ffs, hz, z, logits,
         cand, ehat,
         u_states, u_m, u_ehat, u_delta, u_psi, smp_cfg, smp_u, codes, tgt_rows, nar_logits,
-        delta, psi, slots, out_tok, out_cnt, hist, bm_rows, bm_state, bm_hist, bm_tab, bm_plan, bm_plan_bytes, total;
+        delta, psi, slots, out_tok, out_cnt, hist, bm_rows, bm_state, bm_hist, bm_tab, bm_plan, bm_plan_bytes, bm_sel, bm_sel_bytes, total;
     int64_t m_pre, m_dec, m_max, max_tiles, max_splits, maxp, num_pages;
     int act_bytes;
 };
@@ -204,7 +204,8 @@ WsLayout ws_layout(const mtp_config& c) {
     w.tgt_rows = take(nar ? w.m_pre * 4 : 0);                         // NAR: rows of the target positions
     w.nar_logits = take(nar ? (uint64_t)KH * w.m_pre * (V - 1) * 4 : 0);   // NAR: every stage's logits
     // beam search (mtp_beam_advance): eight arrays of a word per row, the
-    // plan's small outputs, the rows' next state, history and table
+    // plan's small outputs, the rows' next state, history and table, and what
+    // the plan and the selection ask for
     w.bm_rows = take(nar ? 0 : (uint64_t)(8 * B + (B + 1) + 3 * B + 4) * 4);
     w.bm_state = take(nar ? 0 : B * sizeof(SeqState));
     w.bm_hist = take(nar ? 0 : B * (int64_t)c.max_new * 4);
@@ -216,6 +217,16 @@ WsLayout ws_layout(const mtp_config& c) {
         (void)mtp_pages_plan_workspace_size(&pa, &w.bm_plan_bytes);   // (a pool it refuses is refused by the call)
     }
     w.bm_plan = take(w.bm_plan_bytes);
+    // the selection's scratch, for whatever number of beams the search has
+    w.bm_sel_bytes = 0;
+    for (int64_t W = 1; !nar && W <= std::min<int64_t>(32, B); ++W) {
+        mtp_beam_args sa{};
+        sa.n_requests = (int32_t)(B / W); sa.beams = (int32_t)W; sa.vocab = c.vocab; sa.eos_id = c.eos_id;
+        uint64_t bytes = 0;
+        (void)mtp_beam_select_workspace_size(&sa, &bytes);            // (in range for every valid config)
+        w.bm_sel_bytes = std::max(w.bm_sel_bytes, bytes);
+    }
+    w.bm_sel = take(w.bm_sel_bytes);
     w.total = o;
     return w;
 }
@@ -1230,6 +1241,7 @@ int mtp_beam_advance(mtp_ctx* c, int beams, float alpha, int32_t* out_tokens, in
     s.logits = c->ws_ptr<float>(c->ws.logits); s.ld = cf.vocab; s.score = r.score; s.len = r.len; s.done = r.done;
     // (the lengths and marks before the choice are what the rows' parents have: the new ones go elsewhere)
     s.out_score = r.score; s.out_len = skip; s.out_done = small; s.out_parent = w + 5 * B; s.out_token = w + 6 * B;
+    s.workspace = c->WS() + c->ws.bm_sel; s.workspace_bytes = c->ws.bm_sel_bytes;
     int rc = mtp_beam_select(&s, c->stream);
     if (rc) { c->err = "beam selection failed"; return rc; }
     HIPCHK(c, beam_rows_follow(c->stream, r), "beam rows");

@@ -183,3 +183,11 @@ def test_beam_search_after_and_between_other_calls():
         if EOS_ID not in hist[c]:
             assert np.abs(oracle_logits_at(model, phons[c], acs[c], hist[c], 1)[0] - lg[c, 0]).max() <= 1e-4, c
     s.close()
+
+
+@pytest.mark.parametrize("dtype,R,W,tol", [("f32", 2, 16, 1e-4), ("f32", 2, 17, 1e-4), ("f32", 1, 32, 1e-4), ("bf16", 3, 32, 3e-2)])
+def test_beam_search_of_many_beams(dtype, R, W, tol):
+    """Up to the 32 beams that the call takes, where the selection needs a workspace (more than 16) and where it does not."""
+    wl, model, s, phons, acs = _setup(dtype, R, W, 2, 256, eos_lift=0.0, max_new=30)
+    _search(wl, model, s, phons, acs, R, W, 19, tol, check={1, 18})
+    s.close()
