@@ -107,7 +107,7 @@ __device__ __forceinline__ AttnTile find_item(const mtp_attention_args& a, const
     const int s = start_of(a, c), e = start_of(a, c + 1), kv = keys_of(a, c);
     const int count = lane < a.n_rows && e > s ? (e - s + g.tt - 1) / g.tt : 0;
     // what a tile sees of them (in a window from a multiple of 32 on, as runs_of cuts it)
-    const int see = a.window > 0 ? min(kv, min(a.window, 1 << 21) + g.tt + 31) : kv;
+    const int see = a.window > 0 ? min(kv, a.window + g.tt + 31) : kv;
     const int whole = min(see / g.split_len, g.n_splits), rest = whole < g.n_splits ? see - whole * g.split_len : -1;
     const int c0 = count * whole, c1 = rest >= 0 ? count : 0;
     int b0 = 0, b1 = 0, all0 = 0;                // items before this lane's whole runs and before its rest
@@ -1048,8 +1048,11 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream) {
     using namespace mtp;
     const int rc = attn_check(args);
     if (rc != MTP_OK) return rc;
-    const mtp_attention_args& a = *args;
+    mtp_attention_args a = *args;
     if (a.n_rows == 0 || a.n_tokens == 0) return MTP_OK;
+    // (a window of all that a row can hold hides nothing, and a larger one would carry the first position that a query
+    // before the row's start sees, pos - window + 1, out of 32 bits)
+    a.window = std::min(a.window, PG * a.max_pages);
     const int64_t per = a.cache.dtype == MTP_DTYPE_BF16 ? 8 : 4, row = (int64_t)a.n_heads * a.cache.head_dim;
     if (!aligned(a.table, 4) || !aligned(a.row_start, 4) || !aligned(a.kv_len, 4) || !aligned(a.q, 16) ||
         !aligned(a.out, 16) || a.q_stride < row || a.out_stride < row || a.q_stride % per || a.out_stride % per)

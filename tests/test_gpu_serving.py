@@ -879,3 +879,16 @@ def test_attention_many_tokens(HQ, H, D, dtype):
             want = p @ vv
             tol = tol + np.abs(want) * (2.0 ** -8 if bf else 2.0 ** -24)
             assert (np.abs(out[start[c] + pos, h] - want) <= tol).all(), (c, pos, h)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("HQ,H,D,kv,q_len", [(2, 2, 64, [5, 3], [9, 40]), (4, 2, 128, [30, 70], [33, 1]),
+                                             (8, 8, 128, [1000, 700], [1200, 900])])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 3, 2 ** 30])
+def test_attention_windows_wider_than_any_row(window, HQ, H, D, kv, q_len, dtype):
+    """Such a window hides nothing, also of tiles whose first queries sit before the row's start (the last shape is the
+    wide kernel's in bf16): to the bit what the call without a window gives."""
+    c = attention_case(window % 1000, kv, q_len, HQ, H, D, dtype)
+    if max(q_len) < 100:
+        check_attention(c, window=window)
+    assert np.array_equal(run_attention(c, window=window), run_attention(c))
