@@ -334,10 +334,12 @@ __device__ __forceinline__ void beam_merge(const mtp_beam_args& a, int r, const 
     // beam without a finite score or normaliser all -infinity, in token order
     auto candidate = [&](int b, int j, int& tok) {
         double total = -INFINITY;
-        if (s.done[b]) {
+        if (!(fabsf(s.score[b]) < INFINITY)) {
+            tok = j;
+        } else if (s.done[b]) {
             tok = j == 0 ? a.eos_id : (j - 1 < a.eos_id ? j - 1 : j);
-            if (j == 0 && s.score[b] < INFINITY) total = (double)s.score[b];     // (NaN: -infinity too)
-        } else if (!(fabsf(s.score[b]) < INFINITY && fabs(s.lse[b]) < INFINITY)) {
+            if (j == 0) total = (double)s.score[b];
+        } else if (!(fabs(s.lse[b]) < INFINITY)) {
             tok = j;
         } else {
             tok = __float_as_int(s.best[b][j].y);

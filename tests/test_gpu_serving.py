@@ -892,3 +892,22 @@ def test_attention_windows_wider_than_any_row(window, HQ, H, D, kv, q_len, dtype
     if max(q_len) < 100:
         check_attention(c, window=window)
     assert np.array_equal(run_attention(c, window=window), run_attention(c))
+
+
+@pytest.mark.parametrize("W,V", [(4, 9), (4, 500), (7, 7), (16, 40), (20, 2100)])
+def test_beam_select_finished_beams_without_a_score(W, V):
+    """A finished beam whose score is -infinity, NaN or +infinity has candidates of -infinity only, in token order like
+    every other beam's of that kind; too few others are finite, so that some of them are chosen."""
+    rng = np.random.default_rng(W * V)
+    lg = rng.standard_normal((6, W, V)).astype(np.float32)
+    lg[:, W - 1, 2:] = -INF                                # two finite candidates
+    score = -rng.random((6, W)).astype(np.float32)
+    done = np.ones((6, W), np.int32)
+    done[:, W - 1] = 0
+    for r, x in enumerate((-INF, NAN, INF)):
+        score[r, :W - 1] = x                               # all of the finished
+        score[3 + r, 0] = x                                # the first only
+    score[3:, 1:] = -INF
+    score[5] = NAN                                         # nothing at all
+    for eos in (0, 3, V - 1):
+        check_beams(lg, score, rng.integers(1, 9, (6, W)), done, eos, alpha=0.5)
