@@ -123,16 +123,13 @@ __device__ __forceinline__ void beam_chunk(const mtp_beam_args& a, int row, int 
     mine = pl_lo32(bound, other);
     bound = min_f(mine, other);
     const float m = wave_max64(top);
-    // sums of eight exponentials in float32, their sums in float64 (a chunk without a finite logit adds 0)
+    // float32 exponentials, summed in float64 (16 requests of 8 beams over 65,536 logits 20.6 us; 20.3 us with float32
+    // sums of eight, which lose what is below 2^-24 of the largest); a chunk without a finite logit adds 0
     const float mm = m == -INFINITY ? 0.f : m;
-    double sum = 0.0;
+    double part[4] = {0.0, 0.0, 0.0, 0.0};       // (four chains of additions)
 #pragma unroll
-    for (int i = 0; i < NV; i += 8) {
-        float e = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e += __builtin_amdgcn_exp2f((f[i + j] - mm) * LOG2E);
-        sum += (double)e;
-    }
+    for (int i = 0; i < NV; ++i) part[i & 3] += (double)__builtin_amdgcn_exp2f((f[i] - mm) * LOG2E);
+    double sum = (part[0] + part[1]) + (part[2] + part[3]);
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     if (lane == 0) { *mx_out = m; *sum_out = sum; }
 

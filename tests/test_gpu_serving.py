@@ -911,3 +911,21 @@ def test_beam_select_finished_beams_without_a_score(W, V):
     score[5] = NAN                                         # nothing at all
     for eos in (0, 3, V - 1):
         check_beams(lg, score, rng.integers(1, 9, (6, W)), done, eos, alpha=0.5)
+
+
+@pytest.mark.parametrize("V", [449, 1985, 4000, 40000])
+def test_beam_select_sums_exponentials_in_float64(V):
+    """One logit of 0, every 64th behind it -18, the others -infinity (a lane's own logits are 64 apart): the best
+    score is -log1p(n e^-18), which float32 sums around 1 would lose (e^-18 < 2^-25).  It is wrong by the exponentials'
+    relative error, 2^-22 of their own and 2^-24 * 18 * log2(e) + 2^-24 * 18 of their argument, and float64 log's
+    rounding of a sum near 1, 2^-52, beside the output's."""
+    lg = np.full((2, 2, V), -INF, np.float32)
+    lg[:, :, ::64] = -18.0
+    lg[:, :, 0] = 0.0
+    got = serving().select_beams(dev(lg, torch.float32), torch.zeros((2, 2), device="cuda"), dev(np.ones((2, 2))),
+                                 dev(np.zeros((2, 2))), V - 2)
+    n = (V + 63) // 64 - 1
+    want = -np.log1p(n * np.exp(-18.0))
+    s = host(got.score).astype(np.float64)
+    assert (np.abs(s - want) <= -want * (2.0 ** -22 + 2.0 ** -24 * (18 * 2.45 + 1)) + 2.0 ** -52).all(), (s, want)
+    assert (host(got.token) == 0).all() and host(got.parent).tolist() == [[0, 1], [2, 3]]
