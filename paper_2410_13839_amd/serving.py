@@ -103,12 +103,16 @@ def _device(t: torch.Tensor, name: str) -> torch.device:
     return t.device
 
 
+def _no_gradient(t: torch.Tensor, name: str) -> None:
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: the serving operators have no backward pass (call them under torch.no_grad)")
+
+
 def _cache(pool: torch.Tensor) -> _b.mtp_cache:
     if pool.dim() != 4 or pool.dtype not in _DTYPE or not pool.is_contiguous():
         raise ValueError("pool: a contiguous float32 or bfloat16 tensor [pages, 2, kv heads, 16 * head dim]")
     pages, two, heads, block = pool.shape
-    if pool.requires_grad and torch.is_grad_enabled():
-        raise ValueError("pool: the serving operators have no backward pass (call them under torch.no_grad)")
+    _no_gradient(pool, "pool")
     if two != 2 or block not in (PAGE * 64, PAGE * 128):
         raise ValueError(f"pool: [pages, 2, kv heads, 16 * 64 or 16 * 128], not {tuple(pool.shape)}")
     return _b.mtp_cache(pool.data_ptr(), _DTYPE[pool.dtype], pages, heads, block // PAGE)
@@ -124,8 +128,7 @@ def _rows(t: torch.Tensor, name: str, pool: torch.Tensor, dim: int, heads: Optio
     s0, s1, s2 = t.stride()
     if shape[0] and (s2 != 1 or (s1 != dim and shape[1] > 1)):
         raise ValueError(f"{name}: a token's heads must be contiguous")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name}: the serving operators have no backward pass (call them under torch.no_grad)")
+    _no_gradient(t, name)
     return s0 if shape[0] > 1 else shape[1] * dim
 
 
@@ -181,8 +184,10 @@ def write_pages(pool: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: tor
 def copy_pages(pools: torch.Tensor, copies: torch.Tensor) -> None:
     """Copies the pages that a plan's `copies` names, in one layer's pool or,
     with a leading dimension, in every layer's (mtp_pages_copy)."""
+    _need(pools.dim() in (4, 5) and pools.dtype in _DTYPE and pools.is_contiguous(),
+          "pools: a contiguous float32 or bfloat16 tensor [layers,] [pages, 2, kv heads, 16 * head dim]")
+    _no_gradient(pools, "pools")
     dev = _device(pools, "pools")
-    _need(pools.dim() in (4, 5) and pools.is_contiguous(), "pools: contiguous, [layers,] pages, 2, kv heads, 16 * head dim")
     layers = pools.shape[0] if pools.dim() == 5 else 1
     pages = pools.shape[-4]
     page_bytes = pools.shape[-3] * pools.shape[-2] * pools.shape[-1] * pools.element_size()

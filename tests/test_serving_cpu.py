@@ -296,3 +296,20 @@ def test_attention_of_nothing_needs_nothing(n_rows, n_tokens, head_dim, dtype):
     assert b.mtp_pages_attention_workspace_size(a) == 0
     a.workspace = a.workspace_bytes = 0
     b.mtp_pages_attention(a, 0)
+
+
+@pytest.mark.parametrize("shape", [(4, 2, 1, 1024), (3, 4, 2, 1, 1024)])
+def test_copies_in_pools_of_the_wrong_kind_are_refused(shape):
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_amd import serving
+    copies = torch.full((1, 2), -1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="backward"):
+        serving.copy_pages(torch.zeros(shape, requires_grad=True), copies)
+    for dtype in (torch.float16, torch.float64, torch.int32, torch.uint8):
+        with pytest.raises(ValueError, match="float32 or bfloat16"):
+            serving.copy_pages(torch.zeros(shape, dtype=dtype), copies)
+    for t in (torch.zeros(shape), torch.zeros(shape, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError, match="on a GPU"):     # (the kind is right)
+            serving.copy_pages(t, copies)
+    with torch.no_grad(), pytest.raises(ValueError, match="on a GPU"):
+        serving.copy_pages(torch.zeros(shape, requires_grad=True), copies)
