@@ -238,7 +238,8 @@ def select_beams(logits: torch.Tensor, score: torch.Tensor, length: torch.Tensor
     _need(logits.dim() == 3 and logits.dtype == torch.float32, "logits: float32 [requests, beams, vocab]")
     r, w, v = logits.shape
     ld = logits.stride(1) if w > 1 else (logits.stride(0) if r > 1 else v)
-    _need(not (logits.requires_grad and torch.is_grad_enabled()), "logits: no backward pass (call under torch.no_grad)")
+    _no_gradient(logits, "logits")
+    _no_gradient(score, "score")
     _need(v == 0 or logits.stride(2) == 1 or v == 1, "logits: a row's logits must be contiguous")
     _need(r <= 1 or w <= 1 or logits.stride(0) == w * ld, "logits: the rows must be evenly spaced")
     _need(score.dtype == torch.float32 and tuple(score.shape) == (r, w) and score.device == dev and score.is_contiguous(),

@@ -929,3 +929,13 @@ def test_beam_select_sums_exponentials_in_float64(V):
     s = host(got.score).astype(np.float64)
     assert (np.abs(s - want) <= -want * (2.0 ** -22 + 2.0 ** -24 * (18 * 2.45 + 1)) + 2.0 ** -52).all(), (s, want)
     assert (host(got.token) == 0).all() and host(got.parent).tolist() == [[0, 1], [2, 3]]
+
+
+def test_beam_scores_that_need_a_gradient_are_refused():
+    lg, score = torch.zeros((1, 2, 5), device="cuda"), torch.zeros((1, 2), device="cuda")
+    i = torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    for a, b in ((lg, score.clone().requires_grad_()), (lg.clone().requires_grad_(), score)):
+        with pytest.raises(ValueError, match="backward"):
+            serving().select_beams(a, b, i, i, 4)
+        with torch.no_grad():
+            assert host(serving().select_beams(a, b, i, i, 4).token).tolist() == [[0, 1]]
