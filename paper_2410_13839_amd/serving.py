@@ -27,6 +27,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import binding as _b
 
@@ -106,6 +107,9 @@ def _device(t: torch.Tensor, name: str) -> torch.device:
 def _no_gradient(t: torch.Tensor, name: str) -> None:
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: the serving operators have no backward pass (call them under torch.no_grad)")
+    # (the level, -1 outside dual_level, spares a call 0.25 us a tensor)
+    if _forward._current_level >= 0 and _forward.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name}: the serving operators have no forward-mode derivative (unpack_dual gives the primal)")
 
 
 def _cache(pool: torch.Tensor) -> _b.mtp_cache:

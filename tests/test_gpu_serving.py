@@ -939,3 +939,25 @@ def test_beam_scores_that_need_a_gradient_are_refused():
             serving().select_beams(a, b, i, i, 4)
         with torch.no_grad():
             assert host(serving().select_beams(a, b, i, i, 4).token).tolist() == [[0, 1]]
+
+
+def test_calls_with_tangents_are_refused():
+    import torch.autograd.forward_ad as fwd
+    c = attention_case(2, [40], [3], 4, 2, 64, torch.float32)
+    q, pool = c["q"][:3].cuda().view(3, 4, 64), c["pool"].cuda()
+    where = dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"])
+    k, slots = torch.zeros((3, 2, 64), device="cuda"), dev([1, 2, 3])
+    lg, score = torch.zeros((1, 2, 5), device="cuda"), torch.zeros((1, 2), device="cuda")
+    i = torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    before = pool.clone()
+    with fwd.dual_level():
+        d = lambda t: fwd.make_dual(t, torch.ones_like(t))
+        s = serving()
+        for call in (lambda: s.attend_pages(pool, *where, d(q)), lambda: s.attend_pages(d(pool), *where, q),
+                     lambda: s.attend_pages(pool, *where, q, out=d(q.clone())), lambda: s.write_pages(pool, slots, d(k), k),
+                     lambda: s.write_pages(pool, slots, k, d(k)), lambda: s.copy_pages(d(pool), dev([[0, 1]])),
+                     lambda: s.select_beams(d(lg), score, i, i, 4), lambda: s.select_beams(lg, d(score), i, i, 4)):
+            with pytest.raises(ValueError, match="forward-mode"):
+                call()
+        assert torch.equal(pool.view(torch.int32), before.view(torch.int32))   # (NaN behind the keys)
+        s.attend_pages(pool, *where, q)                    # (plain tensors inside dual_level)

@@ -313,3 +313,27 @@ def test_copies_in_pools_of_the_wrong_kind_are_refused(shape):
             serving.copy_pages(t, copies)
     with torch.no_grad(), pytest.raises(ValueError, match="on a GPU"):
         serving.copy_pages(torch.zeros(shape, requires_grad=True), copies)
+
+
+def test_tensors_with_a_tangent_are_refused():
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_amd import serving
+    import torch.autograd.forward_ad as fwd
+    pool, q, copies = torch.zeros(4, 2, 1, 1024), torch.zeros(3, 1, 64), torch.full((1, 2), -1, dtype=torch.int32)
+    calls = {"pool": lambda t: serving._cache(t), "q": lambda t: serving._rows(t, "q", pool, 64),
+             "pools": lambda t: serving.copy_pages(t, copies)}
+    with fwd.dual_level():
+        for name, t in (("pool", pool), ("q", q), ("pools", pool)):
+            dual = fwd.make_dual(t, torch.ones_like(t))
+            with pytest.raises(ValueError, match=f"{name}: .* forward-mode"):
+                calls[name](dual)
+            with torch.no_grad(), pytest.raises(ValueError, match="forward-mode"):   # (no_grad does not stop tangents)
+                calls[name](dual)
+        assert serving._cache(pool).num_pages == 4 and serving._rows(q, "q", pool, 64) == 64
+        assert serving._cache(fwd.unpack_dual(fwd.make_dual(pool, pool)).primal).num_pages == 4
+
+    def f(t):
+        serving._rows(t, "q", pool, 64)
+        return t
+    with pytest.raises(ValueError, match="forward-mode"):
+        torch.func.jvp(f, (q,), (q,))
