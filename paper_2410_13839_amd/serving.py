@@ -7,8 +7,9 @@ torch and enqueues one library call on torch's current stream of the tensors'
 device; nothing is copied to the host and nothing waits, so the calls can be
 captured into a graph.  Tensors made on another stream must be ordered before
 the call by the caller, as for any torch operation.  A refused call raises
-ValueError (a tensor of the wrong kind) or MTPError (the library's own checks)
-with nothing launched.
+ValueError (a tensor of the wrong kind, or a call inside torch.jit.trace, whose
+graph cannot hold it) or MTPError (the library's own checks) with nothing
+launched.
 
 A step of a served batch:
 
@@ -98,7 +99,13 @@ def _workspace(size, args, device):
     return ws
 
 
+_is_tracing = getattr(torch._C, "_is_tracing", None) or torch.jit.is_tracing
+
+
 def _device(t: torch.Tensor, name: str) -> torch.device:
+    """The device that a call's tensors have to share; every call begins here."""
+    if _is_tracing():                            # (a trace would hold the output's allocation and not what fills it)
+        raise ValueError("the serving operators cannot be traced")
     if not t.is_cuda:
         raise ValueError(f"{name}: a tensor on a GPU, not on {t.device}")
     return t.device

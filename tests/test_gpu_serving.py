@@ -961,3 +961,12 @@ def test_calls_with_tangents_are_refused():
                 call()
         assert torch.equal(pool.view(torch.int32), before.view(torch.int32))   # (NaN behind the keys)
         s.attend_pages(pool, *where, q)                    # (plain tensors inside dual_level)
+
+
+def test_calls_inside_a_trace_are_refused():
+    c = attention_case(2, [40], [3], 4, 2, 64, torch.float32)
+    q = c["q"][:3].cuda().view(3, 4, 64)
+    args = c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"])
+    with pytest.raises(ValueError, match="traced"):
+        torch.jit.trace(lambda x: serving().attend_pages(*args, x), (q,))
+    assert torch.isfinite(serving().attend_pages(*args, q)).all()

@@ -337,3 +337,18 @@ def test_tensors_with_a_tangent_are_refused():
         return t
     with pytest.raises(ValueError, match="forward-mode"):
         torch.func.jvp(f, (q,), (q,))
+
+
+def test_calls_inside_a_trace_are_refused():
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_amd import serving
+    pool, i = torch.zeros(4, 2, 1, 1024), torch.zeros((1, 2), dtype=torch.int32)
+    k, f = torch.zeros(2, 1, 64), torch.zeros(1, 2)
+    calls = (lambda x: serving.plan_pages(i[0, :1], i[0, :1], i, 8, 4), lambda x: serving.write_pages(pool, i[0], k, k),
+             lambda x: serving.copy_pages(pool, i), lambda x: serving.attend_pages(pool, i, i[0], i[0, :1], k),
+             lambda x: serving.select_beams(torch.zeros(1, 2, 5), f, i, i, 4))
+    for call in calls:
+        with pytest.raises(ValueError, match="traced"):
+            torch.jit.trace(lambda x: (call(x), x)[1], (f,))
+        with pytest.raises(ValueError, match="on a GPU"):
+            call(f)
