@@ -5,7 +5,8 @@ and the page copies of beams (include/mtp.h's mtp_pages_* and mtp_beam_*).
 Each function checks its tensors, allocates its outputs and workspace with
 torch and enqueues one library call on torch's current stream of the tensors'
 device; nothing is copied to the host and nothing waits, so the calls can be
-captured into a graph.  Tensors made on another stream must be ordered before
+captured into a graph.  What a call writes into a caller's tensor counts as an
+in-place change of it (its version moves on).  Tensors made on another stream must be ordered before
 the call by the caller, as for any torch operation.  A refused call raises
 ValueError (a tensor of the wrong kind, or a call inside torch.jit.trace, whose
 graph cannot hold it) or MTPError (the library's own checks) with nothing
@@ -29,6 +30,7 @@ from typing import NamedTuple, Optional
 
 import torch
 from torch.autograd import forward_ad as _forward
+from torch.autograd.graph import increment_version as _changed
 
 from . import binding as _b
 
@@ -177,6 +179,8 @@ def plan_pages(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, num
         positions.fill_(-1)
     else:
         _launch(_b.mtp_pages_plan, args, dev)
+        if out_table is not None:
+            _changed(out_table)
     return PagePlan(new, row_start, kv_len, slots, positions, copies.view(n, 2), status)
 
 
@@ -190,6 +194,7 @@ def write_pages(pool: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: tor
     _need(k.shape[0] == v.shape[0], "k and v: the same number of tokens")
     p = _ints(slots, "slots", (k.shape[0],), dev)
     _launch(_b.mtp_pages_write, _b.mtp_write_args(cache, k.shape[0], p, k.data_ptr(), v.data_ptr(), ks, vs), dev)
+    _changed(pool)
 
 
 def copy_pages(pools: torch.Tensor, copies: torch.Tensor) -> None:
@@ -206,6 +211,7 @@ def copy_pages(pools: torch.Tensor, copies: torch.Tensor) -> None:
     p = _ints(copies, "copies", (copies.shape[0], 2), dev)
     _launch(_b.mtp_pages_copy, _b.mtp_copy_args(pools.data_ptr(), page_bytes, pages * page_bytes, _i32(layers, "layers"), pages,
                                                 _i32(copies.shape[0], "copies"), p), dev)
+    _changed(pools)
 
 
 def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor,
@@ -223,7 +229,8 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
     qs = _rows(q, "q", pool, dim)
     _need(table.dim() == 2, "table: [rows, max_pages]")
     n, m = table.shape
-    if out is None:
+    own = out is None
+    if own:
         out = torch.empty_like(q)                # (contiguous, as a token's heads are)
         os = q.shape[1] * dim
     else:
@@ -236,6 +243,8 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
                                  _ints(kv_len, "kv_len", (n,), dev), q.data_ptr(), out.data_ptr(), qs, os, None, 0)
     ws = _workspace(_b.mtp_pages_attention_workspace_size, args, dev)
     _launch(_b.mtp_pages_attention, args, dev)
+    if not own:
+        _changed(out)
     return out
 
 

@@ -970,3 +970,33 @@ def test_calls_inside_a_trace_are_refused():
     with pytest.raises(ValueError, match="traced"):
         torch.jit.trace(lambda x: serving().attend_pages(*args, x), (q,))
     assert torch.isfinite(serving().attend_pages(*args, q)).all()
+
+
+def test_what_calls_write_counts_as_changed():
+    """The written tensors' versions move on, views of them and inference tensors included, so that a backward pass that
+    saved one says so; what a call only reads keeps its version."""
+    s = serving()
+    pools = torch.zeros((2, 9, 2, 2, 1024), device="cuda")
+    x = torch.ones(1, device="cuda", requires_grad=True)
+    k, slots, q = torch.ones((3, 2, 64), device="cuda"), dev([1, 2, 3]), torch.ones((3, 4, 64), device="cuda")
+    table, start, kv = dev([[0, 1]]), dev([0, 3]), dev([20])
+    buf = torch.zeros((5, 4, 64), device="cuda")
+    length = dev([3])
+    calls = {"write": (pools, lambda: s.write_pages(pools[1], slots, k, k)),
+             "copy": (pools, lambda: s.copy_pages(pools, dev([[0, 1]]))),
+             "attend": (buf, lambda: s.attend_pages(pools[0], table, start, kv, q, out=buf[1:4])),
+             "plan": (table, lambda: s.plan_pages(length, dev([1]), table, 9, 2, out_table=table))}
+    reads = (k, slots, q, start, kv, length)
+    for name, (t, call) in calls.items():
+        old, olds = t._version, [r._version for r in reads]
+        saved = (x * t.float()).sum() if t.dtype == torch.float32 else None
+        call()
+        assert t._version > old and [r._version for r in reads] == olds, name
+        if saved is not None:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                saved.backward()
+    with torch.inference_mode():
+        p = torch.zeros((9, 2, 2, 1024), device="cuda")
+        s.write_pages(p, slots, k, k)
+        assert float(p.sum()) == 3 * 2 * 2 * 64
+        s.attend_pages(p, table, start, kv, q, out=torch.empty_like(q))
