@@ -160,6 +160,11 @@ __device__ __forceinline__ uint32_t finite2(uint32_t v) {
     const bool lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
     return v & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
 }
+// 0 times two bf16: 0, or NaN where one is not finite.
+__device__ __forceinline__ uint32_t zero_times2(uint32_t v) {
+    const bool lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
+    return (lo ? 0x7fc0u : 0u) | (hi ? 0x7fc00000u : 0u);
+}
 // The larger magnitudes, halves apart, of two pairs of bf16 bits (`most`
 // without signs); a half of 0x7f80 or more is not finite.
 __device__ __forceinline__ uint32_t larger2(uint32_t most, uint32_t v) {
@@ -533,7 +538,8 @@ constexpr int KB = 64;                           // keys of a block
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
-template <int D>
+// ZERO: scale 0, in a kernel of its own (as a branch in one kernel it cost every call 4 to 20%, by the registers around it).
+template <int D, bool ZERO>
 __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_attention_args a, AttnGeo g) {
     constexpr float MSTEP = 8.0f;
     constexpr int CW = D / 8;                    // 16-byte pieces of a K row
@@ -571,14 +577,14 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_tile_kernel(mtp_att
     // (before the queries' loads: loads return in order, and the keys' wait for these)
     int pg_now = pages(0), pg_next = pages(16);
     const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(t.t0 + row / g.gs) * a.q_stride + (hk * group + h0 + hq) * D + 8 * hh;
-    // scores are S x c with c > 0: a negative scale turns the queries' signs, scale 0 their values to 0
-    const float c = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
+    // scores are S x c with c > 0: a negative scale turns the queries' signs, scale 0 (ZERO) their values to 0 times them
+    const float c = ZERO ? 1.f : fabsf(a.scale) * LOG2E;
     bf16x8_t q[D / 16];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
         u32x4_t v = *reinterpret_cast<const u32x4_t*>(qp + 16 * j);
-        if (a.scale < 0.f) v ^= 0x80008000u;
-        if (a.scale == 0.f) v = u32x4_t{0, 0, 0, 0};
+        if (ZERO) v = u32x4_t{zero_times2(v[0]), zero_times2(v[1]), zero_times2(v[2]), zero_times2(v[3])};
+        else if (a.scale < 0.f) v ^= 0x80008000u;
         q[j] = __builtin_bit_cast(bf16x8_t, v);
     }
     // what this lane's row sees; what some row of the wave sees; what every row of the tile sees
@@ -940,7 +946,8 @@ int rows_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
 template <int D>
 int tile_go(hipStream_t st, const mtp_attention_args& a, const AttnGeo& g) {
     const unsigned work = (unsigned)(g.n_tiles * a.cache.n_kv_heads * g.hb);
-    hipLaunchKernelGGL((attn_tile_kernel<D>), dim3(work * g.n_splits), dim3(256), 0, st, a, g);
+    if (a.scale == 0.f) hipLaunchKernelGGL((attn_tile_kernel<D, true>), dim3(work * g.n_splits), dim3(256), 0, st, a, g);
+    else hipLaunchKernelGGL((attn_tile_kernel<D, false>), dim3(work * g.n_splits), dim3(256), 0, st, a, g);
     join_go<bf16_t, D, TR>(st, a, g, work);
     return hipGetLastError() == hipSuccess ? MTP_OK : MTP_EHIP;
 }

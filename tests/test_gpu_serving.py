@@ -1000,3 +1000,25 @@ def test_what_calls_write_counts_as_changed():
         s.write_pages(p, slots, k, k)
         assert float(p.sum()) == 3 * 2 * 2 * 64
         s.attend_pages(p, table, start, kv, q, out=torch.empty_like(q))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 0.125, -0.125])
+@pytest.mark.parametrize("HQ,H,D,q", [(2, 2, 64, 3), (8, 8, 128, 900)])
+def test_attention_queries_that_are_not_numbers(HQ, H, D, q, scale, dtype):
+    """A query that holds a NaN or an infinity (0 x infinity included, so also with scale 0) gets NaN in that head, its
+    neighbours what they get without it; the second shape is the wide kernel's in bf16."""
+    c = attention_case(11, [1000], [q], HQ, H, D, dtype)
+    want = run_attention(c, scale=scale)[:q].reshape(q, HQ, D)
+    assert np.isfinite(want).all()
+    hit = np.zeros((q, HQ), bool)
+    x = c["q"][:q].view(q, HQ, D)
+    for i, (t, h, d, value) in enumerate([(0, 0, 5, NAN), (1, 1, D - 1, NAN), (2, 0, 9, INF), (q - 1, HQ - 1, 0, -INF)]):
+        x[t, h, d] = value
+        hit[t, h] = True
+    got = run_attention(c, scale=scale)[:q].reshape(q, HQ, D)
+    if scale == 0:
+        assert np.isnan(got[hit]).all()
+    else:                                                  # (infinite scores: NaN, or none but -infinite ones: zeros)
+        assert np.isnan(got[hit][[0, 1]]).all()
+    assert np.array_equal(got[~hit], want[~hit])
