@@ -608,15 +608,17 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream);
  * at length len[w] + 1, with eos_id masked (before the softmax) while len[w] <
  * eos_min; a finished beam's only one is itself, as token eos_id with its
  * score and length kept.  The request's next beams are its `beams` best
- * candidates by score / max(length, 1)^alpha, the best first; equal ones in
- * the order of b * vocab + v.  A logit that is NaN counts as -infinity, and so
+ * candidates by score / max(length, 1)^alpha, the best first.  A beam's own
+ * are ordered by their logits, also where float64 rounds their scores to one
+ * value, and equal logits by token; equal candidates of two beams go in the
+ * order of the beams.  A logit that is NaN counts as -infinity, and so
  * does a candidate whose score is NaN or +infinity; candidates of -infinity
- * come last.
+ * come last, a beam's by token.
  * Scores and ranks are formed in float64 from float32 exponentials summed in
- * float64; a beam's own candidates are ordered by their logits.  Written per next
- * beam: out_score (float32), out_len, out_done (done before, or the token is
- * eos_id), out_parent (the row w it continues, as mtp_pages_plan's parent) and
- * out_token.  The out arrays may be the in arrays of the same name.
+ * float64.  Written per next beam: out_score (float32), out_len, out_done (done
+ * before, or the token is eos_id), out_parent (the row w it continues, as
+ * mtp_pages_plan's parent) and out_token.  The out arrays may be the in arrays
+ * of the same name.
  * 0 <= n_requests, n_requests * beams <= 65535, 1 <= beams <= 32, 1 <= vocab
  * < 2^24, ld >= vocab, eos_id in [0, vocab), alpha in [0, 32]; logits
  * 4-byte, workspace 256-byte aligned (NULL when the size call reports 0). */

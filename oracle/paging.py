@@ -149,11 +149,12 @@ def beams(logits, score, length, done, eos, eos_min=0, alpha=0.0):
                 total = np.float64(score[r, b]) + lp
             total = np.where(total < np.inf, total, -np.inf)             # NaN too
             rank = total / max(n, 1) ** float(np.float32(alpha))
-            # the best W of the beam are enough (stable: equal ones by token)
-            for v in np.argsort(-rank, kind="stable")[:W]:
-                cand.append((-rank[v], b * V + int(v), total[v], n, b, int(v)))
-        cand.sort(key=lambda c: c[:2])
-        for i, (_, _, s, n, b, v) in enumerate(cand[:W]):
+            # the best W of the beam are enough: by rank, of equal ones (rounded alike) by logit, then by token
+            key = np.zeros(V) if done[r, b] else np.where(np.isfinite(total), x, 0.0)
+            for i, v in enumerate(np.lexsort((np.arange(V), -key, -rank))[:W]):
+                cand.append((-rank[v], b, i, total[v], n, int(v)))
+        cand.sort(key=lambda c: c[:3])
+        for i, (_, b, _, s, n, v) in enumerate(cand[:W]):
             out[0][r, i] = s
             out[1][r, i] = n
             out[2][r, i] = int(bool(done[r, b]) or v == eos)

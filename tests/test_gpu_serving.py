@@ -1022,3 +1022,17 @@ def test_attention_queries_that_are_not_numbers(HQ, H, D, q, scale, dtype):
     else:                                                  # (infinite scores: NaN, or none but -infinite ones: zeros)
         assert np.isnan(got[hit][[0, 1]]).all()
     assert np.array_equal(got[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("W,V", [(3, 5), (4, 300), (7, 2500), (16, 400), (32, 9000)])
+def test_beam_select_scores_that_rounding_makes_equal(W, V):
+    """Scores of -1e30 swallow the log probabilities in float64: a beam's own candidates still go by their logits."""
+    rng = np.random.default_rng(W + V)
+    lg = (rng.standard_normal((3, W, V)) * 2).astype(np.float32)
+    lg[1] = np.round(lg[1])                                # and many equal logits
+    score = np.full((3, W), -1e30, np.float32)
+    score[2] = -np.float32(1e30) * rng.integers(1, 3, W).astype(np.float32)
+    got = check_beams(lg, score, np.ones((3, W)), np.zeros((3, W)), V - 1)
+    for r in range(2):
+        assert (host(got.parent)[r] == r * W).all()
+        assert host(got.token)[r].tolist() == np.lexsort((np.arange(V), -lg[r, 0]))[:W].tolist()

@@ -352,3 +352,12 @@ def test_calls_inside_a_trace_are_refused():
             torch.jit.trace(lambda x: (call(x), x)[1], (f,))
         with pytest.raises(ValueError, match="on a GPU"):
             call(f)
+
+
+def test_oracle_beams_that_rounding_makes_equal():
+    """1e30 swallows the log probabilities: a beam's own by logit then token, the earlier beam first."""
+    lg = np.array([[[0.0, 2.0, 1.0, 2.0, -INF], [5.0, 4.0, 3.0, 2.0, 1.0], [0.0, 0.0, 9.0, 0.0, 0.0]]], np.float32)
+    for score, parent, token in (([-1e30, -1e30, -1e30], [0, 0, 0], [1, 3, 2]), ([-2e30, -1e30, -INF], [1, 1, 1], [0, 1, 2]),
+                                 ([-INF, -INF, -1e30], [2, 2, 2], [2, 0, 1]), ([-INF, NAN, INF], [0, 0, 0], [0, 1, 2])):
+        out = paging.beams(lg, np.array([score], np.float32), np.ones((1, 3)), np.zeros((1, 3)), 4)
+        assert out[3].tolist() == [parent] and out[4].tolist() == [token]
