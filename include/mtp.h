@@ -567,10 +567,12 @@ int mtp_pages_copy(const mtp_copy_args* args, void* hip_stream);
  *                    (itself included);
  *   MTP_ATTN_FULL    every query sees all kv_len positions (cross attention to
  *                    an encoder's states, or a bidirectional block).
- * A query that sees nothing gets zeros.  Positions in a page outside [0,
- * num_pages) are seen by nobody, and what is not seen never matters, infinite
- * or NaN; a value that is seen and infinite or NaN makes its dimension of the
- * output so, however small its weight.  Tokens outside every row keep what out holds.  Lengths are clamped
+ * A query that sees nothing, or only keys whose scores are -infinity, gets
+ * zeros; one with a score that is NaN or +infinity gets NaN.  Positions in a
+ * page outside [0, num_pages) are seen by nobody, and what is not seen never
+ * matters, infinite or NaN; a value that is seen and infinite or NaN makes its
+ * dimension of the output so, however small its weight.  Tokens outside every
+ * row keep what out holds.  Lengths are clamped
  * to [0, 16 * max_pages], row_start to [0, n_tokens]; row_start must not
  * decrease.  max_kv is a hint, the longest kv_len to expect (0: 16 *
  * max_pages): it sizes the split of the keys over workgroups, and longer rows

@@ -117,8 +117,8 @@ def attend(pool, transposed, table, row_start, kv_len, q, out, causal=True, wind
                 x = q[t, h].astype(np.float64)
                 k, v = ks[seen, h // (HQ // H)], vs[seen, h // (HQ // H)]
                 s = scale * (k @ x)
-                w = np.exp(s - s.max())
-                w /= w.sum()
+                w = np.exp(s - (s.max() if s.max() != -np.inf else 0.0))
+                w /= w.sum() if w.sum() != 0 else 1.0       # (scores of -infinity only: zeros)
                 out[t, h] = w @ v
                 if bound is not None:
                     bound[0][t, h] = w @ np.abs(v)

@@ -1036,3 +1036,42 @@ def test_beam_select_scores_that_rounding_makes_equal(W, V):
     for r in range(2):
         assert (host(got.parent)[r] == r * W).all()
         assert host(got.token)[r].tolist() == np.lexsort((np.arange(V), -lg[r, 0]))[:W].tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,q_len,max_kv", [([40, 300], [1, 3], 0), ([2000, 700], [1, 1], 0), ([1500, 900], [140, 200], 0),
+                                             ([3000], [130], 600)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_scores_of_infinity(D, kv, q_len, max_kv, dtype):
+    """Keys of -infinity in a dimension where the queries are positive score -infinity, those of +infinity infinity.
+    All keys of the first row but the last few score -infinity: they have no weight.  Then all of its first head do:
+    zeros; and one of its second head scores infinity: NaN."""
+    c = attention_case(5, kv, q_len, 2, 2, D, dtype, nan_behind=False)
+    pages, T = c["pool"].shape[0], c["T"]
+    kp = c["pool"][:, 0].view(pages, 2, 16, D)
+    x = c["q"][:T].view(T, 2, D)
+    x[:, :, 0] = x[:, :, 0].abs() + 0.1                    # dimension 0: positive
+    low = kv[0] - q_len[0] - 2                             # positions of the first row that score -infinity, in both heads
+    for j in range(low):
+        kp[c["table"][0, j // 16], :, j % 16, 0] = -INF
+    tame = c["pool"].clone()
+    tame[:, 0] = torch.where(torch.isinf(tame[:, 0]), 0.0, tame[:, 0].float()).to(dtype)
+    qn = c["q"].float().numpy()[:, :2 * D].reshape(-1, 2, D)
+    args = (dtype == torch.bfloat16, c["table"], c["row_start"], c["kv_len"], qn[:T])
+    want, bound, unused = np.zeros((T, 2, D)), np.zeros((2, T, 2, D)), np.zeros((2, T, 2, D))
+    with np.errstate(invalid="ignore"):
+        paging.attend(c["pool"].float().numpy(), *args, want, bound=unused)
+        paging.attend(tame.float().numpy(), *args, np.zeros((T, 2, D)), bound=bound)
+    # (check_attention's tolerance, the scores' error from the finite keys)
+    u = 2.0 ** -24
+    bf = dtype == torch.bfloat16
+    ds = (D + 8) * u * bound[1] + 4 * u
+    tol = unused[0] * (2 * ds + 1100 * u + (2.0 ** -8 if bf else 0.0)) + np.abs(want) * (2.0 ** -8 if bf else u) + 1e-30
+    got = run_attention(c, max_kv=max_kv)[:T].reshape(T, 2, D)
+    assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all()
+    for j in range(low, kv[0]):
+        kp[c["table"][0, j // 16], 0, j % 16, 0] = -INF
+    kp[c["table"][0, 3 // 16], 1, 3, 0] = INF
+    got = run_attention(c, max_kv=max_kv)[:T].reshape(T, 2, D)
+    assert (got[:q_len[0], 0] == 0).all() and np.isnan(got[:q_len[0], 1]).all()
+    assert np.isfinite(got[q_len[0]:]).all()
