@@ -1075,3 +1075,13 @@ def test_attention_scores_of_infinity(D, kv, q_len, max_kv, dtype):
     got = run_attention(c, max_kv=max_kv)[:T].reshape(T, 2, D)
     assert (got[:q_len[0], 0] == 0).all() and np.isnan(got[:q_len[0], 1]).all()
     assert np.isfinite(got[q_len[0]:]).all()
+
+
+@pytest.mark.parametrize("kv,q_len,HQ,H,D,dtype,window", [
+    ([32768], [128], 1, 1, 128, torch.bfloat16, 0), ([65536], [128], 1, 1, 64, torch.bfloat16, 0),
+    ([40000, 17000, 300], [90, 100, 40], 2, 1, 128, torch.bfloat16, 0), ([131072], [1], 1, 1, 64, torch.bfloat16, 0),
+    ([90000, 70000, 20], [2, 1, 1], 4, 1, 64, torch.float32, 0), ([80000], [3], 1, 1, 128, torch.float32, 70001),
+    ([66000], [2], 8, 1, 128, torch.bfloat16, 0)])
+def test_attention_many_runs(kv, q_len, HQ, H, D, dtype, window):
+    """Rows of more than 64 runs, which a lane of a join takes several of (up to 256 runs, the second shape)."""
+    check_attention(attention_case(sum(kv) % 97, kv, q_len, HQ, H, D, dtype), window=window)
