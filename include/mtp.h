@@ -528,7 +528,8 @@ int mtp_pages_plan(const mtp_plan_args* args, void* hip_stream);
 /* Writes the keys and values of n_tokens tokens into the cache: token t's
  * head h, k[t * k_stride + h * head_dim ..] and v likewise, in the cache's
  * type, at slots[t]; a slot outside [0, 16 * num_pages) is skipped.  Slots
- * must differ (two equal ones are left with a mixture of their tokens).
+ * must differ (two equal ones are left with a mixture of their tokens); k and
+ * v must not overlap the pool.
  * Strides are in elements, at least n_kv_heads * head_dim; k, v and the
  * strides' bytes are multiples of 16; ceil(n_tokens / 48) * n_kv_heads < 2^24. */
 typedef struct mtp_write_args {

@@ -10,11 +10,11 @@
 // (a few dozen logits) and taken best first.  A request's workgroup then merges
 // the sorted lists of each beam's chunks, and the beams' lists in float64.  With
 // few chunks all of it is one launch.
-// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 10.4 us
-// for the chunks (3.2 TB/s; 4096 waves load at once and then compute) and 7.7 us
+// What bounds it: 16 requests of 8 beams over 65,536 logits (34 MB) take 11.0 us
+// for the chunks (3.1 TB/s; 4096 waves load at once and then compute) and 7.7 us
 // for the merge, a chain of loads, a float64 exponential, logarithm and power, and
 // eight rounds of a wave maximum per beam.  A beam's lists are merged head by
-// head, a lane a chunk (1 request of 8 beams over 131,072 logits 14.9 us; 28.8 us
+// head, a lane a chunk (1 request of 8 beams over 131,072 logits 15.5 us; 28.8 us
 // with all entries compared every round).  One request of
 // 4 beams over 1025 logits 8 us: the launch and the same chain.
 #include <hip/hip_runtime.h>

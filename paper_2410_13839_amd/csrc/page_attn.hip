@@ -194,11 +194,16 @@ __device__ __forceinline__ uint32_t inside2(int y, int lo, int hi) {
 // transposed V block.  fp32 (16 keys a product): the contraction's index g of
 // step e is dimension 16 j + 4 g + e, or key 4 g + e, and row r of the output
 // tile dt is dimension (D / 16) r + dt, all 16-byte loads again.
+// bf16: probabilities are rounded to bf16, as the matrix product takes them, their
+// sum is not (error against 64 bits 1.8e-3 to 1.9e-3 of the output, 1.6e-3 to
+// 1.7e-3 with float32 probabilities, nearly all of it the output's own rounding).
+// A second product with what the rounding left would take that away, but an
+// infinite value times a remainder of 0 or below would end as NaN.
 //
 // What bounds it: HBM where there are many keys (32 single tokens over 512 to
 // 16,384 keys, 1.1 GB: 210 us, 5.3 TB/s, what a large copy reaches; 220 us with
 // the runs in the rows' order), the chain of loads lengths -> table -> keys and
-// the second launch where there are few (4 tokens over 1075 keys of 16 heads 8.8
+// the second launch where there are few (4 tokens over 1075 keys of 16 heads 8.4
 // us; with 16 waves a head in one launch 11.8 us: a CU alone draws 25 to 50 GB/s).
 constexpr int NW = 4;
 
@@ -531,7 +536,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows_kernel(mtp_attention_arg
 // 64, 8 prompts of 450 tokens 20.2 us.  Pages of a part-seen block that no row of
 // the wave sees are left out, scores and values: chunks over 8192 keys 302 us
 // instead of 314 us.
-// Head dim 64 with four workgroups a CU instead of three: 230 -> 199 us.
+// Head dim 64 with four workgroups a CU instead of three: 230 -> 199 us.  It has
+// 128 registers a lane for them and spills 7 (32 bytes of scratch), stored once
+// before the loops; blocks at the edge of what is seen read some of them back and
+// a refill of the page numbers one, the loop over whole blocks none.
 constexpr int TR = 128;                          // query rows of a tile
 constexpr int KB = 64;                           // keys of a block
 

@@ -9,8 +9,8 @@
 // In all but the largest plans every row's workgroup finds out by itself what
 // the others keep, so that the three steps are one launch.
 // What bounds it: the chain of dependent loads (parent -> lengths -> table ->
-// marks) and the launches, not bytes: 8 rows of 229 pages 6.4 us, 256 beams of
-// 256 pages 13.5 us, 256 rows of 512 15.2 us in three launches.
+// marks) and the launches, not bytes: 8 rows of 229 pages 6.2 us, 256 beams of
+// 256 pages 13.5 us, 256 rows of 512 15.8 us in three launches.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -27,8 +27,8 @@ constexpr int PLAN_T = 256;            // threads of the other two
 // One launch up to these sizes: table entries, pages (a byte of LDS each) and
 // rows (a workgroup each, so one or two a CU).  64 rows of 64 pages 7.4 us instead
 // of 11.3 us in three launches, 256 of 256 (beams) 13.5 and 14.8 us, 256 of 512
-// 20.6 and 15.2 us.  Workgroups of 256 threads, whose sums are shorter, for few
-// pieces of 64 entries: 8 rows of 229 pages 6.4 us, 7.8 us with 1024 threads; 256
+// 20.6 and 15.8 us.  Workgroups of 256 threads, whose sums are shorter, for few
+// pieces of 64 entries: 8 rows of 229 pages 6.2 us, 7.8 us with 1024 threads; 256
 // rows of 16 pages 14.7 and 10.2 us.
 constexpr int ONE_ENTRIES = 1 << 16, ONE_PAGES = 1 << 17, ONE_ROWS = 256, FEW_PIECES = 64;
 
