@@ -6,11 +6,11 @@ Each function checks its tensors, allocates its outputs and workspace with
 torch and enqueues one library call on torch's current stream of the tensors'
 device; nothing is copied to the host and nothing waits, so the calls can be
 captured into a graph.  What a call writes into a caller's tensor counts as an
-in-place change of it (its version moves on).  Tensors made on another stream must be ordered before
-the call by the caller, as for any torch operation.  A refused call raises
-ValueError (a tensor of the wrong kind, or a call inside torch.jit.trace, whose
-graph cannot hold it) or MTPError (the library's own checks) with nothing
-launched.
+in-place change of it (its version moves on).  Tensors made on another stream
+must be ordered before the call by the caller, as for any torch operation.  A
+refused call raises ValueError (a tensor of the wrong kind, or a call inside
+torch.jit.trace, whose graph cannot hold it) or MTPError (the library's own
+checks) with nothing launched.
 
 A step of a served batch:
 
@@ -105,7 +105,7 @@ _is_tracing = getattr(torch._C, "_is_tracing", None) or torch.jit.is_tracing
 
 
 def _device(t: torch.Tensor, name: str) -> torch.device:
-    """The device that a call's tensors have to share; every call begins here."""
+    """The device that a call's tensors have to share; every call asks for it before it allocates or launches."""
     if _is_tracing():                            # (a trace would hold the output's allocation and not what fills it)
         raise ValueError("the serving operators cannot be traced")
     if not t.is_cuda:
