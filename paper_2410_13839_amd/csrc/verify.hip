@@ -380,7 +380,8 @@ __device__ __forceinline__ int token_at(const mtp_verify_args& a, const Judged& 
     const int v0 = ch * 64 * NV + (int)threadIdx.x * EACH;
     double own[EACH], sum = 0.0;
     if (wave < PW) {
-        const float *xp = a.logits + (int64_t)j.t * a.ld, *yp = DRAWN ? a.draft + (int64_t)j.t * a.draft_ld : xp;
+        // (the draft's row where one was refused: behind a row's last token there is none)
+        const float *xp = a.logits + (int64_t)j.t * a.ld, *yp = DRAWN && j.refused ? a.draft + (int64_t)j.t * a.draft_ld : xp;
         float x[EACH], y[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
