@@ -190,3 +190,23 @@ def test_evict_refuses():
     call()
     assert pool._version > before[0] and w._version > before[1]
     assert s.evict_pages(pool, w[:, :0], table[:0], n[:0], 8, 2).shape == (0,)
+
+
+@pytest.mark.parametrize("ties", [False, True])
+@pytest.mark.parametrize("n,budget,recent", [(2064, 1000, 10), (2064, 2063, 0), (2900, 2000, 800), (3001, 700, 7), (4096, 2048, 0),
+                                             (4112, 3000, 16), (4112, 17, 16), (4100, 4099, 64)])
+def test_evict_rows_of_two_to_four_thousand(n, budget, recent, ties):
+    """Tables whose older tokens number 2049 to 4096, both ends among them."""
+    c = case(3 * n, [n, 2100, 40, min(n, 2900)], 1, 2, 64, torch.bfloat16, ties)
+    assert 2048 < 16 * c["table"].shape[1] - recent <= 4096
+    check(c, budget, recent, max(budget, 1500))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,budget,recent,limit", [(list(range(20, 100, 2)), 33, 9, 50), (list(range(380, 428, 2)), 350, 300, 351),
+                                                      ([100, 300] * 12, 64, 0, 128)])
+def test_evict_many_units_of_wide_heads(rows, budget, recent, limit, dtype):
+    """Batches of heads of 128 over several layers: more slices than are taken by 1024 threads each."""
+    c = case(6, rows, 3, 4, 128, dtype)
+    assert 3 * len(rows) * 4 * 4 > 1024
+    check(c, budget, recent, limit)
