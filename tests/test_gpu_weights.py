@@ -234,3 +234,32 @@ def test_weights_refuses():
                 w.clone().requires_grad_()):
         with pytest.raises(ValueError):
             serving().attend_pages(*args, weights=bad)
+
+
+@pytest.mark.parametrize("HQ,H,D,kv,q_len", [
+    (32, 8, 128, [500, 260, 130, 700], [130, 129, 130, 1]),      # whole
+    (32, 8, 128, [1030], [70]), (12, 4, 128, [900, 2000], [65, 130]),                # up to four runs of keys, joined
+    (16, 4, 128, [4100], [64]), (36, 2, 128, [3000, 2900], [50, 33]),                # more of them; two blocks of heads
+    (32, 8, 128, [1500, 1000, 40], [9, 8, 10]),                  # few queries a row
+    (8, 8, 64, [1030], [1000]), (8, 8, 64, [4000], [257])])
+def test_weights_many_queries(HQ, H, D, kv, q_len):
+    """Enough work for the attention's kernel for many query rows: heads of 128, and runs of keys in several workgroups."""
+    check(case(3 * (HQ + D), kv, q_len, HQ, H, D, torch.bfloat16))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kw", [dict(causal=False), dict(window=300), dict(scale=0.0), dict(scale=-0.2), dict(scale=0.0, causal=False)])
+def test_weights_many_queries_of_every_form(D, kw):
+    c = case(6, [1100, 600], [300, 290] if D == 64 else [70, 130], 16, 8, D, torch.bfloat16)
+    check(c, **kw)
+    c["table"][0, 3], c["table"][0, 60], c["table"][1, 5] = -1, c["pool"].shape[0], -2 ** 31
+    c["q"][5, 1] = NAN
+    check(c, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("HQ,H,D", [(2, 2, 64), (2, 1, 128)])
+@pytest.mark.parametrize("q", [1, 60])
+def test_weights_of_few_runs(q, HQ, H, D, dtype):
+    """Two to four runs of keys, whose sums go along with the joins or follow them."""
+    check(case(0, [528], [q], HQ, H, D, dtype))
