@@ -248,9 +248,9 @@ def test_weights_many_queries(HQ, H, D, kv, q_len):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("kw", [dict(causal=False), dict(window=300), dict(scale=0.0), dict(scale=-0.2), dict(scale=0.0, causal=False)])
+@pytest.mark.parametrize("kw", [dict(causal=False), dict(window=950), dict(scale=0.0), dict(scale=-0.2), dict(scale=0.0, causal=False)])
 def test_weights_many_queries_of_every_form(D, kw):
-    c = case(6, [1100, 600], [300, 290] if D == 64 else [70, 130], 16, 8, D, torch.bfloat16)
+    c = case(6, [1100, 600], [75, 65], 64, 8, D, torch.bfloat16)
     check(c, **kw)
     c["table"][0, 3], c["table"][0, 60], c["table"][1, 5] = -1, c["pool"].shape[0], -2 ** 31
     c["q"][5, 1] = NAN
