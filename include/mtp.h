@@ -662,7 +662,9 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream);
  *   weights[(c * n_kv_heads + k) * ld + j] += sum of p_tj over the row's queries t
  *                                             and the query heads that read k,
  * p the probabilities of which out is made (float32, before they are rounded for
- * the product with V).  With MTP_ATTN_CAUSAL the row's last positions, its queries'
+ * the product with V; a score of many queries may be formed a second time, its
+ * products added in another order, and then differs by up to head_dim 2^-23 of the
+ * sum of their magnitudes).  With MTP_ATTN_CAUSAL the row's last positions, its queries'
  * own, are new: their weights start from 0, whatever was there.  Positions behind
  * kv_len, and rows without queries, keep theirs; a query whose output is 0 or NaN
  * throughout adds nothing, nor does a position that nobody sees.  Every sum's order

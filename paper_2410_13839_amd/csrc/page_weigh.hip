@@ -119,6 +119,7 @@ __global__ __launch_bounds__(64 * NW) void weigh_kernel(WeighArgs w) {
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+#pragma clang fp contract(off)                   // (the attention rounds the scaled score, too)
                     const int u = 4 * t + e, key = key_of(u);
                     const bool in = ref.y > 0.f && key >= lo && key < hi && there(u);
                     const float p = __builtin_amdgcn_exp2f(sc[e] * scale - ref.x) * ref.y;
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_tile_kernel(WeighArgs w) {
     const bf16_t* pool = (const bf16_t*)a.cache.pool + (size_t)hk * PG * D;
     const int32_t* tab = a.table + (size_t)c * a.max_pages;
     float* out = w.weights + ((size_t)c * H + hk) * w.ld;
-    const float scale = a.scale * LOG2E;
+    const float scale = fabsf(a.scale) * LOG2E;
     const int qsw = D == 128 ? qc & 15 : (qc >> 1) & 7;
 
     for (int b = run; (int64_t)b * BK < kv; b += w.runs) {
@@ -196,6 +197,12 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_tile_kernel(WeighArgs w) {
         const bf16_t* kp = pool + (size_t)max(qc < PG ? x0 : x1, 0) * pstr + (qc % PG) * D + 8 * hh;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) k[j] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * j);
+        // (scores as the attention over many query rows forms them, times a scale that is not negative)
+        if (a.scale < 0.f) {
+            typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) k[j] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, k[j]) ^ 0x80008000u);
+        }
         // the row's queries that see any key of the block: [i0, i1)
         int64_t i0 = 0, i1 = n;
         if (causal) {

@@ -263,3 +263,35 @@ def test_weights_many_queries_of_every_form(D, kw):
 def test_weights_of_few_runs(q, HQ, H, D, dtype):
     """Two to four runs of keys, whose sums go along with the joins or follow them."""
     check(case(0, [528], [q], HQ, H, D, dtype))
+
+
+# (the kernels that form scores again, and the attention's that they go with: the same products in the same order)
+@pytest.mark.parametrize("HQ,H,D,kv,q,dtype", [
+    (4, 2, 64, 300, 3, torch.bfloat16), (4, 2, 128, 600, 1, torch.float32),          # stored
+    (4, 2, 64, 300, 20, torch.bfloat16), (4, 2, 64, 300, 30, torch.float32), (8, 2, 128, 300, 40, torch.float32),
+    (64, 8, 128, 1100, 75, torch.bfloat16), (64, 8, 64, 1100, 130, torch.bfloat16)])  # many query rows
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+def test_weights_of_large_scores(HQ, H, D, kv, q, dtype, scale):
+    """Each query is a key of its own times +-1: its score, 10^8, lies so far above the others that the key gets the whole
+    weight, however the score rounds (steps of 8 at 1.4 x 10^8).  Few query rows: the reference is the key's own score, the
+    weight 1 exactly.  Many: the reference is off by a rounding, the weight e times 1 / e of some e: the quotient's rounding
+    and the product's, 2^-24 each, and one a sum."""
+    c = case(0, [kv], [q], HQ, H, D, dtype)
+    keys = (torch.randn((kv, H, D), generator=torch.Generator().manual_seed(1)) * (3000.0 if D == 64 else 2100.0)).to(dtype)
+    at = torch.arange(kv)
+    c["pool"][:, 0].view(-1, H, 16, D)[torch.tensor(c["table"][0]).long()[at // 16], :, at % 16] = keys
+    rng = np.random.default_rng(2)
+    want = np.zeros((H, kv))
+    for i in range(q):
+        for h in range(HQ):
+            j = int(rng.integers(0, kv - q + i + 1))
+            c["q"][i, h] = keys[j, h // (HQ // H)] * (1 if scale > 0 else -1)
+            want[h // (HQ // H), j] += 1.0
+    k = keys.double()
+    s = torch.einsum("jhd,ihd->hij", k, k) * 0.125
+    gap = torch.diagonal(s, dim1=1, dim2=2)[:, :, None] - s
+    assert (gap + torch.eye(kv).double() * 1e9).min() > 1e6
+    w = torch.zeros(c["weights"].shape, device="cuda")
+    serving().attend_pages(c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"]), c["q"].cuda(), scale=scale,
+                           weights=w)
+    assert (np.abs(w.cpu().numpy()[0, :, :kv] - want) <= want * (2 + want) * (2.0 ** -24 if HQ == 64 else 0.0)).all()
