@@ -81,6 +81,10 @@ __global__ __launch_bounds__(64 * NW) void weigh_kernel(WeighArgs w) {
         x1 = x1 >= 0 && x1 < a.cache.num_pages ? x1 : -1;
         Operand<T, D> k;
         k.load(pool + (size_t)max(x0, 0) * pstr, pool + (size_t)max(x1, 0) * pstr, r, gr);
+        if (a.scale == 0.f) {                    // scores are 0, also where the product would be infinite
+#pragma unroll
+            for (int j = 0; j < D * (int)sizeof(T) / 64; ++j) k.k[0][j] = k.k[1][j] = make_uint4(0, 0, 0, 0);
+        }
         auto key_of = [&](int u) { return kb + (sizeof(T) == 2 ? 8 * gr + u : 16 * (u >> 2) + 4 * gr + (u & 3)); };
         auto there = [&](int u) { return (key_of(u) - kb < PG ? x0 : x1) >= 0 && key_of(u) < kv; };
         // the row's queries that see any of these keys: [i0, i1)
@@ -197,11 +201,15 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_tile_kernel(WeighArgs w) {
         const bf16_t* kp = pool + (size_t)max(qc < PG ? x0 : x1, 0) * pstr + (qc % PG) * D + 8 * hh;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) k[j] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * j);
-        // (scores as the attention over many query rows forms them, times a scale that is not negative)
-        if (a.scale < 0.f) {
+        // (scores as the attention over many query rows forms them, times a scale above 0; of scale 0 they are 0, also where
+        // the product would be infinite)
+        if (a.scale <= 0.f) {
             typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) k[j] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, k[j]) ^ 0x80008000u);
+            for (int j = 0; j < D / 16; ++j) {
+                const u32x4_t v = __builtin_bit_cast(u32x4_t, k[j]);
+                k[j] = __builtin_bit_cast(bf16x8_t, a.scale == 0.f ? u32x4_t{0, 0, 0, 0} : v ^ 0x80008000u);
+            }
         }
         // the row's queries that see any key of the block: [i0, i1)
         int64_t i0 = 0, i1 = n;

@@ -295,3 +295,19 @@ def test_weights_of_large_scores(HQ, H, D, kv, q, dtype, scale):
     serving().attend_pages(c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"]), c["q"].cuda(), scale=scale,
                            weights=w)
     assert (np.abs(w.cpu().numpy()[0, :, :kv] - want) <= want * (2 + want) * (2.0 ** -24 if HQ == 64 else 0.0)).all()
+
+
+@pytest.mark.parametrize("q,D,rows", [(75, 128, 2), (75, 64, 2), (7, 128, 10)])
+def test_weights_of_scale_0_where_products_overflow(q, D, rows):
+    """Scores of scale 0 are 0, though a product would be infinite: out is the mean of the values, the weights are even.
+    (1 over the keys seen, rounded to float32 twice at most, and a rounding a sum)."""
+    c = case(0, [1100] * rows, [q] * rows, 64, 8, D, torch.bfloat16)
+    c["q"] *= 1e20
+    c["pool"][:, 0] *= 1e20
+    w = torch.zeros(c["weights"].shape, device="cuda")
+    out = serving().attend_pages(c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"]), c["q"].cuda(), scale=0.0,
+                                 weights=w)
+    assert torch.isfinite(out).all()
+    seen = np.arange(1100 - q, 1100)[:, None] + 1
+    want = 8 * ((np.arange(1100)[None] < seen) / seen).sum(0)
+    assert (np.abs(w.cpu().numpy()[:, :, :1100] - want) <= want * (8 * q + 1104) * 2.0 ** -24).all()
