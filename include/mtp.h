@@ -667,8 +667,11 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream);
  * sum of their magnitudes).  With MTP_ATTN_CAUSAL the row's last positions, its queries'
  * own, are new: their weights start from 0, whatever was there.  Positions behind
  * kv_len, and rows without queries, keep theirs; a query whose output is 0 or NaN
- * throughout adds nothing, nor does a position that nobody sees.  Every sum's order
- * is fixed.  weights does not overlap another operand; ld >= 16 * max_pages.  The
+ * throughout adds nothing, nor does a position that nobody sees.  Every other query
+ * counts: what a drafted token's gave to older tokens stays when the draft is
+ * refused.  Weights of a sequence's own tokens alone come from a call behind the
+ * verification, with the queries that stay (each row's first `count`) and kv_len the
+ * lengths with them.  Every sum's order is fixed.  weights does not overlap another operand; ld >= 16 * max_pages.  The
  * workspace (in `attention`) is as large as the size call here reports. */
 typedef struct mtp_weigh_args {
     mtp_attention_args attention;

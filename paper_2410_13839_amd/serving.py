@@ -29,11 +29,23 @@ of a bounded length:
 
     plan = plan_pages(length, add, table, num_pages, max_tokens)
     for l in range(layers):
-        q = write_rotated(pools[l], plan.slots, position, q, k, v, freq)
-        o = attend_pages(pools[l], plan.table, plan.row_start, plan.kv_len, q, weights=weights[l])
+        q[l] = write_rotated(pools[l], plan.slots, position, q[l], k, v, freq)
+        o = attend_pages(pools[l], plan.table, plan.row_start, plan.kv_len, q[l])
     step = verify_drafts(logits, tokens, plan.row_start, uniforms, width, draft_logits)
     length += step.count                                # (the next plan takes the refused drafts' pages back)
+    start = pad(step.count.cumsum(0), (1, 0)).int()     # the tokens that stay: each row's first step.count
+    row = bucketize(number, start[1:], right=True).clamp(max=rows - 1)                  # (number: arange(max_tokens))
+    stay = (plan.row_start[row] + number - start[row]).clamp(max=max_tokens - 1)
+    for l in range(layers):
+        attend_pages(pools[l], plan.table, start, length, q[l][stay], weights=weights[l])
     length = evict_pages(pools, weights, plan.table, length, budget, recent)
+
+The weights are added up behind the verification, from the queries that stay, so
+that what evict_pages keeps goes by the row's own tokens and a row with drafts
+keeps what it keeps without.  With weights= in the first attend_pages, which
+spares the second, the refused drafts' queries count as well: what they gave to
+older tokens stays in the sums, and which tokens are kept, and so the row's later
+tokens, depends on guesses that were thrown away.
 
 A plan's positions are places in the cache.  In a row that evict_pages has cut
 they fall behind the tokens' own numbers, which rotary positions go by: such a
@@ -344,7 +356,8 @@ def attend_pages(pool: torch.Tensor, table: torch.Tensor, row_start: torch.Tenso
     with q or the pool.  weights, float32 [rows, kv heads, positions], gets added
     the weight that each cached token got over a row's queries and the KV head's
     query heads; a causal row's own new tokens start from 0
-    (mtp_pages_attention_weights; what evict_pages keeps tokens by)."""
+    (mtp_pages_attention_weights; what evict_pages keeps tokens by).  Every
+    query counts, a draft's that is refused later, too."""
     dev = _device(pool, "pool")
     cache = _cache(pool)
     dim = cache.head_dim

@@ -51,3 +51,143 @@ def test_verify_takes_drafts_without_the_last_token_s_row(V, lens):
     b.mtp_verify_drafts(args, torch.cuda.current_stream().cuda_stream)
     for t, k in zip([out[0]] + out[2:], ("token", "count", "accepted", "done")):
         assert np.array_equal(t.cpu().numpy(), want[k]), k
+
+
+def kept_tokens(plan, count, number):
+    """As serving.py's text has it: the row starts of the tokens that stay, and their places in the step."""
+    rows, size = count.shape[0], number.shape[0]
+    start = torch.nn.functional.pad(count.cumsum(0), (1, 0)).int()
+    row = torch.bucketize(number, start[1:], right=True).clamp(max=rows - 1)
+    return start, (plan.row_start[row] + number - start[row]).clamp(max=size - 1)
+
+
+def kept_step(m, st, drafts, uniforms, add):
+    """test_gpu_speculative_step's step, its weights from the tokens that stay."""
+    import test_gpu_speculative_step as t
+    s = serving()
+    plan = s.plan_pages(st.length, add, st.table, t.PAGES, t.ROWS * t.WIDTH, out_table=st.table)
+    tokens = torch.cat([st.pending[:, None], drafts], 1).reshape(-1)
+    shift = (st.seen - st.length).repeat_interleave(t.WIDTH)
+    positions = torch.where(plan.positions >= 0, plan.positions + shift, plan.positions)
+    x, qs = m.emb[tokens.long()], []
+    for l in range(t.LAYERS):
+        q, k, v = (x @ m.qkv[l]).split([t.H * t.D, t.HK * t.D, t.HK * t.D], 1)
+        q = s.write_rotated(st.pool[l], plan.slots, positions, q.view(-1, t.H, t.D), k.view(-1, t.HK, t.D), v.view(-1, t.HK, t.D),
+                            m.freq[0], magnitude=m.freq[1])
+        qs.append(q)
+        x = x + s.attend_pages(st.pool[l], plan.table, plan.row_start, plan.kv_len, q).view(-1, t.H * t.D)
+    logits = x @ m.head
+    out = s.verify_drafts(logits, tokens, plan.row_start, uniforms, t.WIDTH, temperature=0.9)
+    st.seen += out.count
+    st.length += out.count
+    st.pending.copy_(out.token.gather(1, (out.count.long() - 1)[:, None])[:, 0])
+    start, stay = kept_tokens(plan, out.count, torch.arange(t.ROWS * t.WIDTH, device="cuda"))
+    for l in range(t.LAYERS):
+        s.attend_pages(st.pool[l], plan.table, start, st.length, qs[l][stay], weights=st.weights[l])
+    st.length.copy_(s.evict_pages(st.pool, st.weights, st.table, st.length, t.BUDGET, t.RECENT, limit=t.LIMIT))
+    return logits, out
+
+
+def test_steps_whose_weights_are_the_sequence_s_own():
+    """80 steps against rows in float64 whose weights come from the emitted tokens' queries alone, as a run without drafts
+    adds them up (tolerances as in test_gpu_speculative_step)."""
+    import test_gpu_speculative_step as t
+    m = t.Model(1)
+    st, plain = t.State(), t.Plain(m)
+    add = torch.full((t.ROWS,), t.WIDTH, dtype=torch.int32, device="cuda")
+    refused = evicted = 0
+    for drafts, uniforms in t.inputs(2, 80):
+        guess = np.stack([[plain.pending[r]] * (t.WIDTH - 1) for r in range(t.ROWS)])
+        drafts = np.where(uniforms.reshape(t.ROWS, t.WIDTH)[:, 1:] < 0.5, guess, drafts).astype(np.int32)
+        lg, out = kept_step(m, st, torch.tensor(drafts).cuda(), torch.tensor(uniforms).cuda(), add)
+        got = lg.double().cpu().numpy().reshape(t.ROWS, t.WIDTH, t.V)
+        token, count = out.token.cpu().numpy(), out.count.cpu().numpy()
+        for r in range(t.ROWS):
+            tokens, n = [plain.pending[r]] + drafts[r].tolist(), int(count[r])
+            before = [[[list(e) for e in c] for c in layer] for layer in plain.cache[r]]
+            assert np.abs(got[r] - plain.logits(r, tokens)).max() <= 2e-4
+            plain.cache[r] = before              # once more, without the refused drafts
+            plain.logits(r, tokens[:n])
+            size = len(plain.cache[r][0][0])
+            for layer in plain.cache[r]:
+                for c in layer:
+                    c += [None] * (t.WIDTH - n)  # (settle takes them off)
+            plain.settle(r, token[r].tolist(), n)
+            refused += t.WIDTH - n
+            evicted += len(plain.cache[r][0][0]) < size
+        assert st.length.tolist() == [len(plain.cache[r][0][0]) for r in range(t.ROWS)] and st.seen.tolist() == plain.seen
+        w = st.weights.double().cpu().numpy()
+        for r in range(t.ROWS):
+            for l in range(t.LAYERS):
+                for h in range(t.HK):
+                    have, want = np.sort(w[l, r, h, :int(st.length[r])]), np.sort([e[2] for e in plain.cache[r][l][h]])
+                    assert np.abs(have - want).max() <= 1e-3
+    assert refused >= 100 and evicted >= 3 and plain.closest > 1e-5
+
+
+def test_such_steps_captured_and_replayed():
+    import test_gpu_speculative_step as t
+    m = t.Model(3)
+    data = [(torch.tensor(d).cuda(), torch.tensor(u).cuda()) for d, u in t.inputs(4, 30)]
+    add = torch.full((t.ROWS,), t.WIDTH, dtype=torch.int32, device="cuda")
+    eager, want = t.State(), []
+    for d, u in data:
+        lg, out = kept_step(m, eager, d, u, add)
+        want.append([lg.clone()] + [x.clone() for x in out])
+    st, other = t.State(), t.State()
+    drafts, uniforms = data[0][0].clone(), data[0][1].clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                # (torch's products want a first call before a capture)
+        kept_step(m, t.State(), drafts, uniforms, add)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lg, out = kept_step(m, st, drafts, uniforms, add)
+    for i, (d, u) in enumerate(data):
+        drafts.copy_(d)
+        uniforms.copy_(u)
+        graph.replay()
+        if i % 3 == 0:
+            kept_step(m, other, d, u, add)
+        if i % 5 == 0:
+            torch.cuda.synchronize()
+        for a, b in zip([lg] + list(out), want[i]):
+            assert torch.equal(a, b), i
+    for a, b in zip(st.tensors(), eager.tensors()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_weights_of_refused_drafts(dtype):
+    """What a call adds is every query's, drafts' that are refused later among them; behind the verification, from the
+    queries that stay, it is what a step without drafts adds.  A probability is within 1200 x 2^-24 of itself and twice
+    (D + 8) 2^-24 of its score's magnitudes, below 60 here, in either call, and sums of 8 round 8 times."""
+    rng = np.random.default_rng(4)
+    rows, H, HK, D, w = 3, 8, 2, 64, 5
+    lens = np.array([37, 130, 16])
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pool = torch.randn((30, 2, HK, 16 * D), generator=g, device="cuda").to(dtype)
+    table, length = dev(rng.permutation(30).reshape(rows, 10)), dev(lens)
+    q = torch.randn((rows * w, H, D), generator=g, device="cuda").to(dtype)
+    old = torch.rand((rows, HK, 160), generator=g, device="cuda")
+    number = torch.arange(rows * w, device="cuda")
+
+    class plan:
+        row_start = dev(np.arange(rows + 1) * w)
+
+    def call(start, n, x):
+        sums = old.clone()
+        serving().attend_pages(pool, table, start, n, x, weights=sums)
+        return sums
+
+    single = call(dev(np.arange(rows + 1)), length + 1, q[::w].contiguous())
+    every = call(plan.row_start, length + w, q)
+    count = torch.ones(rows, dtype=torch.int32, device="cuda")
+    start, stay = kept_tokens(plan, count, number)
+    kept = call(start, length + count, q[stay])
+    for r, n in enumerate(lens):
+        tol = 2 * (1200 + 2 * 72 * 60 + 8) * 2.0 ** -24 * 4 + 2.0 ** -24 * 8
+        assert (kept[r, :, :n + 1] - single[r, :, :n + 1]).abs().max() <= tol
+        gone = (every[r, :, :n].double() - single[r, :, :n].double()).sum(-1)
+        # (a query gives its head's sums 1 in all, part of it to its own row's new tokens)
+        assert (gone > 0).all() and (gone < (w - 1) * H // HK).all() and gone.max() > 1.0
