@@ -549,8 +549,9 @@ int mtp_pages_write(const mtp_write_args* args, void* hip_stream);
  * dimensions i and pairs + i, MTP_ROTARY_NEIGHBOURS 2 i and 2 i + 1.  inverse =
  * 1 turns by -a (what a turn by a is undone by, with 1 / magnitude; with the same
  * magnitude the transpose, which a gradient takes).  freq is float64 [pairs],
- * radians per position; angles are formed in float64 (within 2^-50 of
- * themselves and 2^-26), the turn in float32, rounded once to the type. */
+ * radians per position; angles are formed in float64 and rounded to float32 when
+ * they are reduced to [-pi/4, pi/4] (within 2^-50 of themselves and 2^-25), the turn
+ * in float32, rounded once to the type. */
 #define MTP_ROTARY_HALVES      0
 #define MTP_ROTARY_NEIGHBOURS  1
 typedef struct mtp_rotary {

@@ -21,7 +21,7 @@ constexpr int WOWN = 48, WEXT = 7;     // a group's own tokens, tokens looked at
 // Bit i, lane i's token: the first of an octet; in none.
 struct WriteOctets { uint64_t heads, alone; };
 
-// The slots of the group of tokens t0 .. t0 + 47 into s_slot (entry i: token t0 -
+// The slots of the group of tokens t0 .. t0 + WOWN - 1 into s_slot (entry i: token t0 -
 // 7 + i; -1 where there is none), and with TURN its octets, whose entries go to
 // s_oct.  slot_of(t): the slot of token t, by the caller's own rule.  The caller
 // synchronises.
