@@ -672,8 +672,13 @@ int mtp_pages_attention(const mtp_attention_args* args, void* hip_stream);
  * counts: what a drafted token's gave to older tokens stays when the draft is
  * refused.  Weights of a sequence's own tokens alone come from a call behind the
  * verification, with the queries that stay (each row's first `count`) and kv_len the
- * lengths with them.  Every sum's order is fixed.  weights does not overlap another operand; ld >= 16 * max_pages.  The
- * workspace (in `attention`) is as large as the size call here reports. */
+ * lengths with them.  Every sum's order is fixed.  weights does not overlap another
+ * operand; ld >= 16 * max_pages.
+ * The workspace (in `attention`) is as large as the size call here reports.  For few
+ * queries a row it has room for their scores of every place of the table, n_tokens *
+ * n_heads * 16 * max_pages floats, whatever max_kv says, up to 256 MB; where that
+ * would be more they are formed twice, which is slower: a table of the width that the
+ * rows need is the fastest. */
 typedef struct mtp_weigh_args {
     mtp_attention_args attention;
     float* weights;             /* [n_rows][n_kv_heads][ld]                    */

@@ -360,8 +360,11 @@ struct WeighCut {
 
 // Stored where a key has 16 times as many bytes as it has queries, and no more than 256 MB of scores in all (16 single
 // tokens over 4000 keys, four query heads on each of 8 KV heads of 128 in bf16, 64 bytes a query: 53 us stored, 79 us formed
-// again; fp32, head dim 128, 32 queries, 16 bytes: 96 and 98 us; bf16, head dim 64, 8 queries, 16 bytes, 24.4 and 23.3 us,
-// 16 queries 27.5 and 23.9 us).  Else 32 x 32 tiles for bf16 rows of 64 queries and more on average (16 rows over 2000 keys
+// again; at the border, 16 bytes, neither is 5% ahead: fp32, head dim 128, 32 queries 96 and 98 us, bf16, head dim 64, 8
+// queries 24.4 and 23.3 us; past it, bf16, head dim 64, 16 queries 27.5 and 23.9 us).  Their room is that of the table,
+// since max_kv is a hint that a row may exceed: a table far wider than its rows forms them again (32 single tokens over 500
+// to 2000 keys, 32 heads on 8 of 128: 41 us with tables of 125 or 1024 pages, 53 us with 8192, max_kv 2000; 4 tokens a row
+// 65 and 64 us).  Else 32 x 32 tiles for bf16 rows of 64 queries and more on average (16 rows over 2000 keys
 // of 8 heads of 128: 64 queries 59 us in tiles of 32 and 66 us in tiles of 16, 32 queries 64 and 61 us; of 4 heads of 64:
 // 64 queries 31.5 us either way, 32 queries 29.0 and 25.8 us).
 WeighCut weigh_cut(const mtp_attention_args& a) {

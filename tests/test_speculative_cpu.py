@@ -300,3 +300,19 @@ def test_the_documented_bound_of_rotary_angles():
     assert np.abs(y).max() <= math.pi / 4 and 2.0 ** -26 < worst <= 2.0 ** -25
     header = open(os.path.join(os.path.dirname(__file__), "..", "include", "mtp.h")).read()
     assert "within 2^-50 of themselves and 2^-25" in header
+
+
+def test_weights_workspace_follows_the_table():
+    """As documented: room for the scores of every place of the table up to 256 MB, whatever the hint of the rows' length."""
+    b = _b()
+
+    def size(pages, max_kv, tokens=32):
+        a = b.mtp_attention_args(b.mtp_cache(4096, b.MTP_DTYPE_BF16, 10, 8, 128), 32, pages, tokens, 32, b.MTP_ATTN_CAUSAL, 0, max_kv,
+                                 0.1, 256, 256, 256, 256, 256, 4096, 4096, None, 0)
+        return b.mtp_pages_attention_weights_workspace_size(b.mtp_weigh_args(a, 256, 16 * pages))
+
+    scores = lambda pages, tokens=32: tokens * 32 * 16 * pages * 4
+    for max_kv in (0, 2000):
+        assert scores(125) < size(125, max_kv) and scores(1024) < size(1024, max_kv) < 2 * scores(1024)
+        assert scores(4096) == 1 << 28 and size(4096, max_kv) > 1 << 28
+        assert size(4097, max_kv) < 1 << 26 and size(8192, max_kv, 128) < 1 << 28
