@@ -781,8 +781,9 @@ int mtp_beam_select(const mtp_beam_args* args, void* hip_stream);
  * and independent the target's own distribution.
  * temperature 0: p_t is 1 at the largest logit (of equal ones the lowest id),
  * uniforms and draft logits play no part.  eos_id (or -1) is masked in p_t and
- * q_t while len[r] + (t - s) < eos_min; an emitted one ends the row: nothing is
- * emitted behind it.  A logit that is NaN counts as -infinity, infinite ones
+ * q_t while len[r] + (t - s) < eos_min, so that there the drafts have to be drawn
+ * with it masked (else what is emitted is not the target's distribution); an emitted
+ * one ends the row: nothing is emitted behind it.  A logit that is NaN counts as -infinity, infinite ones
  * share the whole, and a row of -infinity alone accepts nothing and gives no
  * token.  A draft outside [0, vocab) is refused.
  * Written per row: token[width] (-1 behind the emitted ones) and prob[width],

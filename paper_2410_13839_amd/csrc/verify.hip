@@ -42,8 +42,8 @@ constexpr int EACH = 8;                          // logits of a lane where a dra
 // Up to this many chunks of 512 of a row's tokens (and draft rows) one launch does everything.  Whole calls in one launch and in
 // two: 16 rows of 4 tokens of 1025 logits, 12 chunks, 9.5 and 10.8 us, of 8 tokens, 24, 10.9 and 10.8, of 10, 30, 12.2 and 11.1,
 // of 16, 48, 14.4 and 11.2; 64 rows, 24 chunks, 11.1 and 11.3, 30, 12.3 and 11.7; one row, 12, 9.1 and 10.0, 24, 10.4 and 10.1
-// (three launches, draft logits, 24 chunks: 11.7 and 12.4; 32: 12.3 either way).  256 rows are faster in one up to 96 and more
-// (48 chunks 15.2 and 19.7).
+// (three launches, draft logits, 24 chunks: 11.7 and 12.4; 32: 12.3 either way).  256 rows are faster in one at every number measured,
+// 96 at most (48 chunks 15.2 and 19.7).
 constexpr int FUSED_UNITS = 24;
 
 // A chunk's, or a row's: its largest logit, the sum of exp((x - max) / T), and with

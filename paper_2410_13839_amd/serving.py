@@ -483,7 +483,9 @@ def verify_drafts(logits: torch.Tensor, tokens: torch.Tensor, row_start: torch.T
     that was decided before and the drafts behind it, `width` in all at most.  uniforms: float32 [tokens] from [0, 1), a
     draft's own for its test and the row's first for the token drawn behind the accepted ones.  draft_logits: what the drafts
     were drawn from, row t the answer to token t like the target's; None for drafts that are certain (a lattice's best path).
-    length: int32 [rows], generated tokens before the step, needed with eos_min > 0."""
+    length: int32 [rows], generated tokens before the step, needed with eos_min > 0.  While a row has fewer than eos_min tokens
+    eos_id is masked in the target's and in the draft's distribution: draw the drafts from logits masked alike, or what is
+    emitted is not the target's distribution."""
     dev = _device(logits, "logits")
     _need(logits.dim() == 2 and row_start.dim() == 1 and row_start.shape[0] >= 1, "logits: [tokens, vocab]; row_start: [rows + 1]")
     t, v = logits.shape
