@@ -789,7 +789,8 @@ int mtp_beam_select(const mtp_beam_args* args, void* hip_stream);
  * Written per row: token[width] (-1 behind the emitted ones) and prob[width],
  * p_t of each emitted token (0 behind), count (emitted tokens), accepted (the
  * drafts accepted, those behind an end too) and done (1: the last emitted token
- * is eos_id).  Exponentials and sums are float64.
+ * is eos_id).  Exponentials and sums are float64; an exponential below 2^-1022 of
+ * the largest may count as 0.
  * 0 <= n_rows <= 4096, 0 <= n_tokens < 2^24, 1 <= vocab < 2^24, ld and draft_ld
  * >= vocab, 1 <= width <= 256, n_rows * width * ceil(vocab / 2048) < 2^24, n_rows
  * * ceil(vocab / 8192) < 2^22; temperature finite, 0 or with a

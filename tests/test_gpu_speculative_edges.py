@@ -221,3 +221,14 @@ def test_verify_masks_the_end_in_both_distributions():
             counts += torch.bincount(got.token[:, 0].long(), minlength=V).cpu().numpy()
         n = counts.sum()
         assert n == 10 * R and (np.abs(counts - n * want) <= 5 * np.sqrt(n * want * (1 - want)) + 1e-6).all()
+
+
+@pytest.mark.parametrize("V", [40, 9000])
+def test_verify_of_the_smallest_shares(V):
+    """With a uniform of 0 a draft passes as long as its exponential is not 0: e^-700 of the largest does, e^-720 is below
+    2^-1022."""
+    x = np.zeros((2, V), np.float32)
+    for gap, accepted in ((700.0, 1), (720.0, 0)):
+        x[0, 5] = gap
+        got = serving().verify_drafts(dev(x, torch.float32), dev([1, 3]), dev([0, 2]), dev([0.5, 0.0], torch.float32), 2)
+        assert got.accepted.tolist() == [accepted] and got.token[0, 0].item() == (3 if accepted else 5)
