@@ -34,7 +34,7 @@ of a bounded length:
     step = verify_drafts(logits, tokens, plan.row_start, uniforms, width, draft_logits)
     length += step.count                                # (the next plan takes the refused drafts' pages back)
     start = pad(step.count.cumsum(0), (1, 0)).int()     # the tokens that stay: each row's first step.count
-    row = bucketize(number, start[1:], right=True).clamp(max=rows - 1)                  # (number: arange(max_tokens))
+    row = bucketize(number, start[1:], right=True).clamp(max=rows - 1)                  # (torch's; number: arange(max_tokens))
     stay = (plan.row_start[row] + number - start[row]).clamp(max=max_tokens - 1)
     for l in range(layers):
         attend_pages(pools[l], plan.table, start, length, q[l][stay], weights=weights[l])

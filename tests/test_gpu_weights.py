@@ -311,3 +311,23 @@ def test_weights_of_scale_0_where_products_overflow(q, D, rows):
     seen = np.arange(1100 - q, 1100)[:, None] + 1
     want = 8 * ((np.arange(1100)[None] < seen) / seen).sum(0)
     assert (np.abs(w.cpu().numpy()[:, :, :1100] - want) <= want * (8 * q + 1104) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("HQ,H,D,kv,q,dtype", [(8, 2, 64, [300, 90], 2, torch.bfloat16), (8, 2, 64, [300, 90], 20, torch.bfloat16),
+                                               (8, 2, 128, [300, 90], 30, torch.float32), (5, 1, 64, [200, 150], 70, torch.bfloat16),
+                                               (32, 8, 128, [900, 400], 90, torch.bfloat16)])
+def test_weights_of_queries_within_a_wider_buffer(HQ, H, D, kv, q, dtype):
+    """Queries from one QKV buffer, an output beside others: the bits of tight ones, and what lies around stays."""
+    c = case(3, kv, [q] * len(kv), HQ, H, D, dtype)
+    args = (c["pool"].cuda(), dev(c["table"]), dev(c["row_start"]), dev(c["kv_len"]))
+    T = c["q"].shape[0]
+    w = dev(c["weights"], torch.float32)
+    out = serving().attend_pages(*args, c["q"].cuda(), weights=w)
+    wide = torch.full((T, (HQ + 2 * H) * D), 3.0, dtype=dtype, device="cuda")
+    wide[:, :HQ * D] = c["q"].cuda().view(T, -1)
+    room = torch.full((T + 1, HQ * D + 16), 7.0, dtype=dtype, device="cuda")
+    w2 = dev(c["weights"], torch.float32)
+    serving().attend_pages(*args, wide[:, :HQ * D].view(T, HQ, D), weights=w2, out=room[:T, 8:8 + HQ * D].view(T, HQ, D))
+    assert torch.equal(w.view(torch.int32), w2.view(torch.int32))
+    assert torch.equal(room[:T, 8:8 + HQ * D].reshape(T, HQ, D), out)
+    assert (room[T:] == 7).all() and (room[:, :8] == 7).all() and (room[:, 8 + HQ * D:] == 7).all() and (wide[:, HQ * D:] == 3).all()
