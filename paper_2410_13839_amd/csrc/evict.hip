@@ -540,7 +540,8 @@ int check(const mtp_evict_args* a) {
 // threads: 512 slices, rows of 2100 to 8000 tokens cut to 2048, 125 and 101 us, of 2300 tokens 50 and 45; 1024 slices, 196 and
 // 188, 64 and 73, of 500 to 8192 tokens 183 and 157, of 4096 to 16,384 tokens 294 and 276; 2048 slices 355 and 338, 177 us either
 // way, of 1152 tokens with 1000 recent 157 and 182; 4096 slices 627 and 608, 325 and 348, 297 and 354 (the moves alone, 12,288
-// slices of rows of up to 1152, half of them cut, 210 and 263 us).  fp32 within 5%, but 4096 slices of 2300 tokens 84 and 105.
+// slices of rows of up to 1152, half of them cut, 210 and 263 us).  fp32 mostly within
+// 5% (up to 6% faster, 12% slower, 4096 slices of 2300 tokens 84 and 105 us).
 constexpr unsigned WIDE_GROUPS = 1024;
 template <typename T, int D>
 int go(hipStream_t st, const mtp_evict_args& a, const EvictWs& w) {
